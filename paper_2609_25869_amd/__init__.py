@@ -8,6 +8,13 @@ the package itself cannot be imported before the library exists).
 
     plan = bsa.plan(mask_dev, head_offset, stride_b, B_Q, B_KV, q, k, v, o)
     bsa.forward(plan, q, k, v, o, lse)          # warm repeats reuse the plan
+
+Rotary positions and window attention (ops.py, libbsa_ops.so,
+include/bsa_ops.h) stand beside them:
+
+    q, k = bsa.rope(q, k, freq=freq, pairs=(22, 21, 21), grid=(32, 45, 80))
+    o, lse = bsa.window_forward(q, k, v, left, right, sinks)
+    dq, dk, dv = bsa.window_backward(q, k, v, o, lse, do, left, right, sinks)
 """
 from __future__ import annotations
 
@@ -20,6 +27,9 @@ from . import _ffi
 from ._ffi import (BsaError, CatalogEntry, Mask, PlanOpts, RegimeQuery, SegmentInfo, Shapes,  # noqa: F401
                    DTYPE_BF16, EXPORT_BH_NNZ, EXPORT_COL_IDX, EXPORT_DISPATCH, EXPORT_ROW_PTR, EXPORT_TASKS,
                    EXPORT_TILE_KV, EXPORT_TILE_MEMBER, EXPORT_TILE_PTR)
+
+from .ops import (ALL, rope, rope_frequencies, window_backward, window_forward,  # noqa: F401
+                  window_workspace)
 
 _lib = _ffi.load()
 

@@ -1,9 +1,9 @@
-"""Build libbsa.so (HIP for gfx950) in-tree with hipcc.
+"""Build libbsa.so and libbsa_ops.so (HIP for gfx950) in-tree with hipcc.
 
 Usage: python paper_2609_25869_amd/build.py [--jobs N]
 
 Run it as a script: importing it through the package would import the
-package, which refuses to load before libbsa.so exists.
+package, which refuses to load before the libraries exist.
 """
 from __future__ import annotations
 
@@ -19,8 +19,10 @@ ROOT = os.path.dirname(HERE)
 CSRC = os.path.join(HERE, "csrc")
 BUILD = os.path.join(HERE, "_build")
 LIB = os.path.join(HERE, "libbsa.so")
+OPS_LIB = os.path.join(HERE, "libbsa_ops.so")
 
 SOURCES = ["runtime.hip", "plan_kernels.hip", "attn_fwd.hip", "sparsify.hip", "task_order.hip", "catalog.cpp"]
+OPS_SOURCES = ["ops_runtime.hip", "rope.hip", "window_fwd.hip", "window_bwd.hip"]
 ARCH = "gfx950"
 
 
@@ -28,7 +30,7 @@ def hipcc() -> str:
     for cand in (os.environ.get("HIPCC"), "/opt/rocm/bin/hipcc", shutil.which("hipcc")):
         if cand and os.path.exists(cand):
             return cand
-    raise RuntimeError("hipcc not found (ROCm is required to build libbsa.so)")
+    raise RuntimeError("hipcc not found (ROCm is required to build the libraries)")
 
 
 def common_flags():
@@ -47,7 +49,9 @@ def common_flags():
 # addend of the exponent and finds masked scores that are not finite by the
 # NaN they give.
 EXTRA_FLAGS = {"attn_fwd.hip": ["-mllvm", "-amdgpu-mfma-vgpr-form"],
-               "sparsify.hip": ["-mllvm", "-amdgpu-mfma-vgpr-form"]}
+               "sparsify.hip": ["-mllvm", "-amdgpu-mfma-vgpr-form"],
+               "window_fwd.hip": ["-mllvm", "-amdgpu-mfma-vgpr-form"],
+               "window_bwd.hip": ["-mllvm", "-amdgpu-mfma-vgpr-form"]}
 
 
 def _compile(src: str) -> str:
@@ -65,18 +69,23 @@ def _compile(src: str) -> str:
     return obj
 
 
-def build(jobs: int = 4, verbose: bool = False) -> str:
-    os.makedirs(BUILD, exist_ok=True)
-    with concurrent.futures.ThreadPoolExecutor(max_workers=max(1, jobs)) as ex:
-        objs = list(ex.map(_compile, SOURCES))
-    tmp = LIB + ".tmp%d" % os.getpid()
+def _link(objs, lib: str):
+    tmp = lib + ".tmp%d" % os.getpid()
     cmd = [hipcc(), "-shared", "-fPIC", "--offload-arch=%s" % ARCH] + objs + ["-o", tmp, "-ldl"]
     r = subprocess.run(cmd, stdout=subprocess.PIPE, stderr=subprocess.STDOUT, text=True)
     if r.returncode != 0:
-        raise RuntimeError("linking libbsa.so failed:\n" + r.stdout)
-    os.replace(tmp, LIB)
+        raise RuntimeError("linking %s failed:\n%s" % (os.path.basename(lib), r.stdout))
+    os.replace(tmp, lib)
+
+
+def build(jobs: int = 4, verbose: bool = False) -> str:
+    os.makedirs(BUILD, exist_ok=True)
+    with concurrent.futures.ThreadPoolExecutor(max_workers=max(1, jobs)) as ex:
+        objs = list(ex.map(_compile, SOURCES + OPS_SOURCES))
+    _link(objs[:len(SOURCES)], LIB)
+    _link(objs[len(SOURCES):], OPS_LIB)
     if verbose:
-        print("built", LIB)
+        print("built", LIB, OPS_LIB)
     return LIB
 
 

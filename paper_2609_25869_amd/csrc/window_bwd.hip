@@ -1,0 +1,388 @@
+// Window attention backward for gfx950, in two kernels and without atomics:
+//
+//   dQ    walks the keys of 128 rows as the forward kernel does, forming the
+//         probabilities again from the scores and the LSE, and also leaves every
+//         row's D = sum(dO o O) and base-2 LSE in the workspace;
+//   dK/dV walks, for 128 keys, the queries that see any of them, head by head.
+//
+//   P = exp(S - LSE), dS = P o (dO V^T - D)
+//   dQ = scale dS K, dV = P^T dO, dK = scale dS^T Q
+//
+// In both a wave holds 32 of its own rows (queries, or keys) as operands in
+// registers, and the products over the head dim come out with one of those per
+// lane, which is the layout that the products over the walked rows need.
+#include "window_common.h"
+
+// (Kernel bodies are kept from the host's pass, which drops the launch stub of a
+// template whose device builtins it cannot check.)
+
+namespace bsa_ops {
+
+namespace {
+
+constexpr int kWaves = 4;
+
+// ---------------------------------------------------------------- dQ
+template <typename T, int D>
+__global__ __launch_bounds__(64 * kWaves) void window_dq_kernel(WindowArgs a) {
+#ifdef __HIP_DEVICE_COMPILE__
+  using E = Elem<T>;
+  using R = Rows<D>;
+  typedef typename E::x8 x8;
+  constexpr int TK = 32, TQ = 32 * kWaves, kStages = 4;
+  constexpr int kTile = TK * R::kBytes;
+  using Load = TileLoad<D, TK, kWaves>;
+  constexpr int kGroup = 2 * Load::kLoads;
+  __shared__ __attribute__((aligned(1024))) uint8_t ring0[2 * kTile];
+  __shared__ __attribute__((aligned(1024))) uint8_t ring1[2 * kTile];
+  __shared__ __attribute__((aligned(1024))) uint8_t ring2[2 * kTile];
+  __shared__ __attribute__((aligned(1024))) uint8_t ring3[2 * kTile];
+  auto slot = [&](int i) -> uint8_t* { return i == 0 ? ring0 : i == 1 ? ring1 : i == 2 ? ring2 : ring3; };
+
+  const int64_t item = item_of_slot(blockIdx.x, (int64_t)a.ntiles * a.B * a.Hkv);
+  const int tile = (int)(item % a.ntiles), bh = (int)(item / a.ntiles);
+  const int b = bh / a.Hkv, kvh = bh % a.Hkv;
+  const Seq sq(a, b);
+  const int nrows = sq.q_len * a.group, r0 = tile * TQ;
+  if (r0 >= nrows) return;
+  KeyTiles kt;
+  kt.init<TK>(a, sq, r0 / a.group, (min(r0 + TQ, nrows) - 1) / a.group);
+
+  const int tid = threadIdx.x, lane = tid & 63;
+  const int w = __builtin_amdgcn_readfirstlane(tid >> 6);
+  const int n = lane & 31, hh = lane >> 5;
+  const int row = r0 + 32 * w + n;
+  const bool live = row < nrows;
+  const int qi = live ? row / a.group : 0, qh = kvh * a.group + (live ? row % a.group : 0);
+  const int lo = sq.lo(a, qi), hi = live ? sq.hi(a, qi) : -1;
+
+  x8 qf[R::kSteps], df[R::kSteps];
+  float delta = 0.f;
+  {
+    const T* qp = static_cast<const T*>(a.q) + b * a.qs.b + qh * a.qs.h + qi * a.qs.n;
+    const T* dp = static_cast<const T*>(a.dout) + b * a.dos.b + qh * a.dos.h + qi * a.dos.n;
+    const T* op = static_cast<const T*>(a.o) + b * a.os.b + qh * a.os.h + qi * a.os.n;
+#pragma unroll
+    for (int c = 0; c < R::kSteps; ++c) {
+      qf[c] = *reinterpret_cast<const x8*>(qp + 16 * c + 8 * hh);
+      df[c] = *reinterpret_cast<const x8*>(dp + 16 * c + 8 * hh);
+      const x8 of = *reinterpret_cast<const x8*>(op + 16 * c + 8 * hh);
+#pragma unroll
+      for (int e = 0; e < 8; ++e) delta += (float)df[c][e] * (float)of[e];
+    }
+    delta += other_half(delta, lane);
+  }
+  const float lse = a.lse[((int64_t)b * a.H + qh) * a.Nq + qi] * kLog2e;
+  if (live && hh == 0) {
+    float* st = a.stats + ((int64_t)b * a.H + qh) * 2 * a.stat_rows + qi;
+    st[0] = lse;
+    st[a.stat_rows] = delta;
+  }
+
+  Load lk, lv;
+  lk.init(a.ks.n, w, lane);
+  lv.init(a.vs.n, w, lane);
+  const char* kb = reinterpret_cast<const char*>(static_cast<const T*>(a.k) + b * a.ks.b + kvh * a.ks.h);
+  const char* vb = reinterpret_cast<const char*>(static_cast<const T*>(a.v) + b * a.vs.b + kvh * a.vs.h);
+  auto issue = [&](int t, uint8_t* s) {
+    const int j = kt.key<TK>(t), rows = t < kt.nt ? kt.limit(t) - j : 0;
+    lk.issue(kb + (int64_t)j * a.ks.n * 2, rows, s, w);
+    lv.issue(vb + (int64_t)j * a.vs.n * 2, rows, s + kTile, w);
+  };
+  int roff[R::kSteps], toff[2][R::kBlocks];
+#pragma unroll
+  for (int c = 0; c < R::kSteps; ++c) roff[c] = R::row_read(lane, c);
+#pragma unroll
+  for (int r = 0; r < 2; ++r) {
+#pragma unroll
+    for (int d = 0; d < R::kBlocks; ++d) toff[r][d] = R::tr_read(lane, r, d);
+  }
+  f32x16 acc[R::kBlocks];
+#pragma unroll
+  for (int d = 0; d < R::kBlocks; ++d) acc[d] = f32x16{};
+  const int wave_last = min(r0 + 32 * w + 31, nrows - 1);
+  const int full_lo = wave_last >= r0 + 32 * w ? sq.lo(a, wave_last / a.group) : kFar;
+  const int full_hi = wave_last >= r0 + 32 * w ? sq.hi(a, (r0 + 32 * w) / a.group) : -1;
+
+  if (kt.nt > 0) {
+#pragma unroll
+    for (int s = 0; s < kStages - 1; ++s) issue(s, slot(s));
+  }
+  for (int t0 = 0; t0 < kt.nt; t0 += kStages) {
+#pragma unroll
+    for (int u = 0; u < kStages; ++u) {
+      const int t = t0 + u;
+      if (t >= kt.nt) break;
+      wait_vm_lgkm<(kStages - 2) * kGroup>();
+      block_sync();
+      issue(t + kStages - 1, slot((u + kStages - 1) % kStages));
+      const uint8_t* ks = slot(u);
+      const uint8_t* vs = ks + kTile;
+      const int j0 = kt.key<TK>(t);
+      f32x16 s = {}, dp = {};
+#pragma unroll
+      for (int c = 0; c < R::kSteps; ++c) {
+        s = E::mfma(*reinterpret_cast<const x8*>(ks + roff[c]), qf[c], s);
+        dp = E::mfma(*reinterpret_cast<const x8*>(vs + roff[c]), df[c], dp);
+      }
+      float ds[16];
+#pragma unroll
+      for (int i = 0; i < 16; ++i) ds[i] = fast_exp2(__builtin_fmaf(s[i], a.scale_log2, -lse)) * (dp[i] - delta);
+      const bool full = (j0 >= full_lo || j0 + TK <= a.sinks) && j0 + TK - 1 <= full_hi;
+      if (!full) {
+        const uint32_t bits = visible_bits(j0, lo, hi, a.sinks) >> (4 * hh);
+#pragma unroll
+        for (int i = 0; i < 16; ++i) ds[i] = (bits >> ((i >> 2) * 8 + (i & 3))) & 1u ? ds[i] : 0.f;
+      }
+      u32x4 p[2];
+#pragma unroll
+      for (int i = 0; i < 16; i += 2) p[i / 8][(i % 8) / 2] = pack2<T>(ds[i], ds[i + 1]);
+#pragma unroll
+      for (int c = 0; c < 2; ++c) {
+#pragma unroll
+        for (int d = 0; d < R::kBlocks; ++d)
+          acc[d] = E::mfma(read_tr_pair<T>(ks + c * 16 * R::kBytes + toff[0][d], ks + c * 16 * R::kBytes + toff[1][d]),
+                           __builtin_bit_cast(x8, p[c]), acc[d]);
+      }
+    }
+  }
+  wait_vm_lgkm<0>();
+  if (!live) return;
+  T* gp = static_cast<T*>(a.dq) + b * a.dqs.b + qh * a.dqs.h + qi * a.dqs.n;
+#pragma unroll
+  for (int d = 0; d < R::kBlocks; ++d) {
+#pragma unroll
+    for (int g = 0; g < 4; ++g) {
+      u32x2 v;
+      v[0] = pack2<T>(acc[d][4 * g] * a.scale, acc[d][4 * g + 1] * a.scale);
+      v[1] = pack2<T>(acc[d][4 * g + 2] * a.scale, acc[d][4 * g + 3] * a.scale);
+      *reinterpret_cast<u32x2*>(gp + d * 32 + 8 * g + 4 * hh) = v;
+    }
+  }
+#endif
+}
+
+// ---------------------------------------------------------------- dK, dV
+// The queries that see key j: i from first(j) to last(j).
+struct Seen {
+  int off, q_last, left, right, sinks, kv_len;
+  __device__ Seen(const WindowArgs& a, const Seq& s)
+      : off(s.off), q_last(s.q_len - 1), left(a.left), right(a.right), sinks(a.sinks), kv_len(s.kv_len) {}
+  __device__ int first(int j) const { return (int)min(max((int64_t)j - right - off, (int64_t)0), (int64_t)kFar); }
+  __device__ int last(int j) const {
+    if (j >= kv_len) return -1;
+    return j < sinks ? q_last : (int)max(min((int64_t)j + left - off, (int64_t)q_last), (int64_t)-1);
+  }
+};
+
+template <typename T, int D>
+__global__ __launch_bounds__(64 * kWaves) void window_dkv_kernel(WindowArgs a) {
+#ifdef __HIP_DEVICE_COMPILE__
+  using E = Elem<T>;
+  using R = Rows<D>;
+  typedef typename E::x8 x8;
+  constexpr int TR = 32, TKEY = 32 * kWaves, kStages = 4;
+  constexpr int kTile = TR * R::kBytes, kStat = 256;
+  using Load = TileLoad<D, TR, kWaves>;
+  constexpr int kGroup = 2 * Load::kLoads + 1;
+  constexpr int kSlot = 2 * kTile + kWaves * kStat;  // Q, dO, and LSE and D of the rows, a copy per wave
+  __shared__ __attribute__((aligned(1024))) uint8_t ring0[kSlot];
+  __shared__ __attribute__((aligned(1024))) uint8_t ring1[kSlot];
+  __shared__ __attribute__((aligned(1024))) uint8_t ring2[kSlot];
+  __shared__ __attribute__((aligned(1024))) uint8_t ring3[kSlot];
+  auto slot = [&](int i) -> uint8_t* { return i == 0 ? ring0 : i == 1 ? ring1 : i == 2 ? ring2 : ring3; };
+
+  const int64_t item = item_of_slot(blockIdx.x, (int64_t)a.nktiles * a.B * a.Hkv);
+  const int tile = (int)(item % a.nktiles), bh = (int)(item / a.nktiles);
+  const int b = bh / a.Hkv, kvh = bh % a.Hkv;
+  const Seq sq(a, b);
+  const int k0 = tile * TKEY;
+  if (k0 >= sq.kv_len) return;
+  const Seen seen(a, sq);
+  // queries that see any key of the tile (a sink's last query is the sequence's last)
+  const int i_lo = seen.first(k0);
+  const int i_hi = k0 < a.sinks ? sq.q_len - 1 : seen.last(min(k0 + TKEY, sq.kv_len) - 1);
+  const int per_head = max(i_hi - i_lo + TR, 0) / TR;  // row tiles
+  const int nt = per_head * a.group;
+
+  const int tid = threadIdx.x, lane = tid & 63;
+  const int w = __builtin_amdgcn_readfirstlane(tid >> 6);
+  const int n = lane & 31, hh = lane >> 5;
+  const int key = k0 + 32 * w + n;
+  const bool live = key < sq.kv_len;
+  const int first = seen.first(key), last = seen.last(key);
+
+  x8 kf[R::kSteps], vf[R::kSteps];
+  {
+    const int at = live ? key : k0;
+    const T* kp = static_cast<const T*>(a.k) + b * a.ks.b + kvh * a.ks.h + at * a.ks.n;
+    const T* vp = static_cast<const T*>(a.v) + b * a.vs.b + kvh * a.vs.h + at * a.vs.n;
+#pragma unroll
+    for (int c = 0; c < R::kSteps; ++c) {
+      kf[c] = *reinterpret_cast<const x8*>(kp + 16 * c + 8 * hh);
+      vf[c] = *reinterpret_cast<const x8*>(vp + 16 * c + 8 * hh);
+    }
+  }
+
+  Load lq, ld;
+  lq.init(a.qs.n, w, lane);
+  ld.init(a.dos.n, w, lane);
+  // the row tile that is loaded next, and the one that is worked on
+  int g_in = 0, i_in = i_lo, i_now = i_lo;
+  const uint32_t stat_off = (uint32_t)(n * 4) + (hh ? (uint32_t)(a.stat_rows * 4) : 0u);
+  auto issue = [&](uint8_t* s) {
+    const bool any = g_in < a.group;
+    const int qh = kvh * a.group + (any ? g_in : 0), rows = any ? i_hi + 1 - i_in : 0;
+    lq.issue(reinterpret_cast<const char*>(static_cast<const T*>(a.q) + b * a.qs.b + qh * a.qs.h + i_in * a.qs.n), rows, s, w);
+    ld.issue(reinterpret_cast<const char*>(static_cast<const T*>(a.dout) + b * a.dos.b + qh * a.dos.h + i_in * a.dos.n), rows,
+             s + kTile, w);
+    const float* st = a.stats + ((int64_t)b * a.H + qh) * 2 * a.stat_rows + i_in;
+    const __amdgpu_buffer_rsrc_t rsrc = __builtin_amdgcn_make_buffer_rsrc(
+        const_cast<float*>(st), 0, any ? (int)((a.stat_rows + TR) * 4) : 0, 0x00020000);
+    __builtin_amdgcn_raw_ptr_buffer_load_lds(
+        rsrc, (__attribute__((address_space(3))) void*)(s + 2 * kTile + w * kStat), 4, stat_off, 0, 0, 0);
+    i_in += TR;
+    if (i_in > i_hi) {
+      i_in = i_lo;
+      ++g_in;
+    }
+  };
+
+  int roff[R::kSteps], toff[2][R::kBlocks];
+#pragma unroll
+  for (int c = 0; c < R::kSteps; ++c) roff[c] = R::row_read(lane, c);
+#pragma unroll
+  for (int r = 0; r < 2; ++r) {
+#pragma unroll
+    for (int d = 0; d < R::kBlocks; ++d) toff[r][d] = R::tr_read(lane, r, d);
+  }
+  f32x16 dk[R::kBlocks], dv[R::kBlocks];
+#pragma unroll
+  for (int d = 0; d < R::kBlocks; ++d) {
+    dk[d] = f32x16{};
+    dv[d] = f32x16{};
+  }
+  // rows of a tile that every key of the wave is seen by
+  const int kw = k0 + 32 * w;
+  const int full_lo = seen.first(kw + 31);
+  const int full_hi = kw + 31 >= sq.kv_len ? -1 : min(seen.last(kw), kw < a.sinks && kw + 31 >= a.sinks ? seen.last(a.sinks) : kFar);
+
+  if (nt > 0) {
+#pragma unroll
+    for (int s = 0; s < kStages - 1; ++s) issue(slot(s));
+  }
+  for (int t0 = 0; t0 < nt; t0 += kStages) {
+#pragma unroll
+    for (int u = 0; u < kStages; ++u) {
+      const int t = t0 + u;
+      if (t >= nt) break;
+      wait_vm_lgkm<(kStages - 2) * kGroup>();
+      block_sync();
+      issue(slot((u + kStages - 1) % kStages));
+      const uint8_t* qs = slot(u);
+      const uint8_t* gs = qs + kTile;
+      const uint8_t* st = qs + 2 * kTile + w * kStat + 16 * hh;
+      f32x16 s = {}, dp = {};
+#pragma unroll
+      for (int c = 0; c < R::kSteps; ++c) {
+        s = E::mfma(*reinterpret_cast<const x8*>(qs + roff[c]), kf[c], s);
+        dp = E::mfma(*reinterpret_cast<const x8*>(gs + roff[c]), vf[c], dp);
+      }
+      const bool full = i_now >= full_lo && i_now + TR - 1 <= full_hi;
+      uint32_t bits = ~0u;
+      if (!full) bits = (bits_below(last - i_now + 1) & ~bits_below(first - i_now)) >> (4 * hh);
+      u32x4 p[2], q[2];
+#pragma unroll
+      for (int r4 = 0; r4 < 4; ++r4) {
+        const f32x4 lse = *reinterpret_cast<const f32x4*>(st + 32 * r4);
+        const f32x4 delta = *reinterpret_cast<const f32x4*>(st + 128 + 32 * r4);
+        float pv[4], dsv[4];
+#pragma unroll
+        for (int e = 0; e < 4; ++e) {
+          const int i = 4 * r4 + e;
+          pv[e] = fast_exp2(__builtin_fmaf(s[i], a.scale_log2, -lse[e]));
+          dsv[e] = pv[e] * (dp[i] - delta[e]);
+          if (!full) {
+            const bool see = (bits >> (8 * r4 + e)) & 1u;
+            pv[e] = see ? pv[e] : 0.f;
+            dsv[e] = see ? dsv[e] : 0.f;
+          }
+        }
+#pragma unroll
+        for (int e = 0; e < 4; e += 2) {
+          p[r4 / 2][(4 * (r4 % 2) + e) / 2] = pack2<T>(pv[e], pv[e + 1]);
+          q[r4 / 2][(4 * (r4 % 2) + e) / 2] = pack2<T>(dsv[e], dsv[e + 1]);
+        }
+      }
+#pragma unroll
+      for (int c = 0; c < 2; ++c) {
+#pragma unroll
+        for (int d = 0; d < R::kBlocks; ++d) {
+          const int o0 = c * 16 * R::kBytes + toff[0][d], o1 = c * 16 * R::kBytes + toff[1][d];
+          dv[d] = E::mfma(read_tr_pair<T>(gs + o0, gs + o1), __builtin_bit_cast(x8, p[c]), dv[d]);
+          dk[d] = E::mfma(read_tr_pair<T>(qs + o0, qs + o1), __builtin_bit_cast(x8, q[c]), dk[d]);
+        }
+      }
+      i_now += TR;
+      if (i_now > i_hi) i_now = i_lo;
+    }
+  }
+  wait_vm_lgkm<0>();
+  if (!live) return;
+  T* kp = static_cast<T*>(a.dk) + b * a.dks.b + kvh * a.dks.h + key * a.dks.n;
+  T* vp = static_cast<T*>(a.dv) + b * a.dvs.b + kvh * a.dvs.h + key * a.dvs.n;
+#pragma unroll
+  for (int d = 0; d < R::kBlocks; ++d) {
+#pragma unroll
+    for (int g = 0; g < 4; ++g) {
+      u32x2 x, y;
+      x[0] = pack2<T>(dk[d][4 * g] * a.scale, dk[d][4 * g + 1] * a.scale);
+      x[1] = pack2<T>(dk[d][4 * g + 2] * a.scale, dk[d][4 * g + 3] * a.scale);
+      y[0] = pack2<T>(dv[d][4 * g], dv[d][4 * g + 1]);
+      y[1] = pack2<T>(dv[d][4 * g + 2], dv[d][4 * g + 3]);
+      *reinterpret_cast<u32x2*>(kp + d * 32 + 8 * g + 4 * hh) = x;
+      *reinterpret_cast<u32x2*>(vp + d * 32 + 8 * g + 4 * hh) = y;
+    }
+  }
+#endif
+}
+
+template <typename T, int D>
+hipError_t launch(const WindowArgs& a, hipStream_t s) {
+  const int64_t nq = (int64_t)a.ntiles * a.B * a.Hkv, nk = (int64_t)a.nktiles * a.B * a.Hkv;
+  if (nq > 0x7fffffff || nk > 0x7fffffff) return hipErrorInvalidValue;
+  if (nq > 0) {
+    hipLaunchKernelGGL((window_dq_kernel<T, D>), dim3((unsigned)nq), dim3(64 * kWaves), 0, s, a);
+    const hipError_t e = hipGetLastError();
+    if (e != hipSuccess) return e;
+  }
+  if (nk > 0) {
+    hipLaunchKernelGGL((window_dkv_kernel<T, D>), dim3((unsigned)nk), dim3(64 * kWaves), 0, s, a);
+    return hipGetLastError();
+  }
+  return hipSuccess;
+}
+
+}  // namespace
+
+BackwardPlan plan_backward(const WindowArgs& a, int) {
+  BackwardPlan p{};
+  const int64_t rows = (int64_t)a.Nq * a.group;
+  p.ntiles = (int32_t)((rows + 32 * kWaves - 1) / (32 * kWaves));
+  p.nktiles = (a.Nkv + 32 * kWaves - 1) / (32 * kWaves);
+  p.stat_rows = ((int64_t)a.Nq + 63) / 32 * 32;
+  p.floats = (int64_t)a.B * a.H * 2 * p.stat_rows + 32;
+  return p;
+}
+
+hipError_t launch_window_backward(int dtype, int d, const WindowArgs& args, hipStream_t s) {
+  WindowArgs a = args;
+  const BackwardPlan p = plan_backward(a, d);
+  a.ntiles = p.ntiles;
+  a.nktiles = p.nktiles;
+  a.stat_rows = p.stat_rows;
+  if (dtype == kBf16) return d == 128 ? launch<__bf16, 128>(a, s) : launch<__bf16, 64>(a, s);
+  return d == 128 ? launch<_Float16, 128>(a, s) : launch<_Float16, 64>(a, s);
+}
+
+}  // namespace bsa_ops

@@ -1,0 +1,205 @@
+"""Host-side checks of libbsa_ops.so (no GPU needed): exported names, structure
+layouts, compiler options, workspace sizes, and every refusal.  A refusal comes
+before any device work, so made-up device addresses serve."""
+import ctypes
+import os
+import re
+import shutil
+import subprocess
+
+import pytest
+
+ROOT = os.path.dirname(os.path.dirname(os.path.abspath(__file__)))
+HEADER = os.path.join(ROOT, "include", "bsa_ops.h")
+
+bsa = pytest.importorskip("paper_2609_25869_amd")
+from paper_2609_25869_amd import _ffi, _ops_ffi  # noqa: E402
+from paper_2609_25869_amd import ops  # noqa: E402
+from tests.test_build_flags import _builder  # noqa: E402
+
+LIB = ops._lib
+PTR = 1 << 20  # 16-byte aligned, never read
+
+
+def test_exports_header_and_binding_agree():
+    names = sorted(set(re.findall(r"^BSA_API\s+[\w\s\*]*?\b(bsa_\w+)\s*\(", open(HEADER).read(), flags=re.M)))
+    out = subprocess.run(["nm", "-D", "--defined-only", _ops_ffi.LIB_PATH], stdout=subprocess.PIPE, text=True,
+                         check=True).stdout
+    assert sorted(l.split()[-1] for l in out.splitlines() if l.split()[1] == "T") == names
+    assert sorted(n for n, _, _ in _ops_ffi.SIGNATURES) == names and len(names) == 5
+
+
+@pytest.mark.skipif(shutil.which("gcc") is None, reason="gcc not available")
+def test_ctypes_layout_matches_the_header(tmp_path):
+    pairs = [("bsa_rope_shapes", _ops_ffi.RopeShapes), ("bsa_window_shapes", _ops_ffi.WindowShapes),
+             ("bsa_window_grads", _ops_ffi.WindowGrads)]
+    lines = ['#include <stdio.h>', '#include <stddef.h>', '#include "bsa_ops.h"', "int main(void) {"]
+    for c, cls in pairs:
+        lines.append('  printf("%s size %%zu\\n", sizeof(%s));' % (c, c))
+        lines += ['  printf("%s %s %%zu\\n", offsetof(%s, %s));' % (c, f, c, f) for f, _ in cls._fields_]
+    (tmp_path / "l.c").write_text("\n".join(lines + ["  return 0;", "}"]) + "\n")
+    subprocess.run(["gcc", "-std=c11", "-I", os.path.join(ROOT, "include"), str(tmp_path / "l.c"), "-o",
+                    str(tmp_path / "l")], check=True)
+    out = subprocess.run([str(tmp_path / "l")], check=True, stdout=subprocess.PIPE, text=True).stdout
+    got = {tuple(l.split()[:2]): int(l.split()[2]) for l in out.splitlines()}
+    for c, cls in pairs:
+        assert got[(c, "size")] == ctypes.sizeof(cls)
+        for f, _ in cls._fields_:
+            assert got[(c, f)] == getattr(cls, f).offset, (c, f)
+
+
+def test_build_options():
+    b = _builder()
+    for src in b.OPS_SOURCES:
+        flags = b.common_flags() + b.EXTRA_FLAGS.get(src, [])
+        assert "-packed-fp32-ops" in flags
+        assert not {"-ffast-math", "-Ofast", "-fno-honor-nans", "-ffinite-math-only"} & set(flags)
+
+
+def contiguous(n, h, d):
+    return (ctypes.c_int64 * 3)(n * h * d, d, h * d)
+
+
+def window(**kw):
+    s = _ops_ffi.WindowShapes()
+    s.batch, s.heads, s.kv_heads, s.seq_q, s.seq_kv, s.head_dim, s.dtype = 2, 4, 2, 100, 120, 128, _ffi.DTYPE_BF16
+    s.left, s.right, s.sinks = 30, 0, 4
+    for f, v in kw.items():
+        if not f.endswith("_stride"):
+            setattr(s, f, v)
+    s.q_stride = s.o_stride = contiguous(max(s.seq_q, 0), s.heads, s.head_dim)
+    s.k_stride = s.v_stride = contiguous(max(s.seq_kv, 0), s.kv_heads, s.head_dim)
+    for f, v in kw.items():
+        if f.endswith("_stride"):
+            setattr(s, f, (ctypes.c_int64 * 3)(*v))
+    return s
+
+
+def forward(s, ptrs=None, ws=PTR, n=1 << 40):
+    p = dict(q=PTR, k=PTR, v=PTR, o=PTR, lse=PTR)
+    p.update(ptrs or {})
+    return LIB.bsa_window_forward(ctypes.byref(s) if s is not None else None, p["q"], p["k"], p["v"], p["o"], p["lse"],
+                                  None, None, ws, n, None)
+
+
+def grads(s, **kw):
+    g = _ops_ffi.WindowGrads()
+    g.do_stride = g.dq_stride = s.q_stride
+    g.dk_stride = g.dv_stride = s.k_stride
+    for f, v in kw.items():
+        setattr(g, f, (ctypes.c_int64 * 3)(*v))
+    return g
+
+
+def backward(s, g, ptrs=None, ws=PTR, n=1 << 40):
+    names = ("q", "k", "v", "o", "lse", "dout", "dq", "dk", "dv")
+    p = dict.fromkeys(names, PTR)
+    p.update(ptrs or {})
+    return LIB.bsa_window_backward(ctypes.byref(s), ctypes.byref(g) if g is not None else None,
+                                   *[p[x] for x in names], None, None, ws, n, None)
+
+
+INVALID, UNSUPPORTED = _ffi.BSA_ERR_INVALID, _ffi.BSA_ERR_UNSUPPORTED
+
+BAD_WINDOW = [
+    (dict(batch=-1), INVALID, "negative"), (dict(seq_q=-1), INVALID, "negative"), (dict(seq_kv=-5), INVALID, "negative"),
+    (dict(heads=0), INVALID, "positive"), (dict(kv_heads=0), INVALID, "positive"), (dict(heads=5), INVALID, "multiple"),
+    (dict(left=-2), INVALID, "left"), (dict(right=-2), INVALID, "left"), (dict(sinks=-1), INVALID, "sinks"),
+    (dict(scale=-1.0), INVALID, "scale"), (dict(scale=float("inf")), INVALID, "scale"),
+    (dict(scale=float("nan")), INVALID, "scale"), (dict(reserved=1), INVALID, "reserved"),
+    (dict(dtype=_ffi.DTYPE_F32), UNSUPPORTED, "bfloat16"), (dict(dtype=7), UNSUPPORTED, "bfloat16"),
+    (dict(head_dim=96), UNSUPPORTED, "head_dim"), (dict(seq_kv=(1 << 29) + 1), UNSUPPORTED, "2^29"),
+    (dict(heads=256, kv_heads=1, seq_q=1 << 23), UNSUPPORTED, "2^30"),
+    (dict(q_stride=(100 * 512, 128, 511)), INVALID, "aligned"), (dict(k_stride=(-1, 128, 256)), INVALID, "negative"),
+    (dict(k_stride=(120 * 256, 128, 1 << 23)), UNSUPPORTED, "token stride"),
+    (dict(o_stride=(100 * 512, 128, 128)), INVALID, "overlap"), (dict(o_stride=(0, 128, 512)), INVALID, "overlap"),
+    (dict(v_stride=(1 << 58, 128, 256)), INVALID, "address"),
+]
+
+
+@pytest.mark.parametrize("kw,status,word", BAD_WINDOW)
+def test_window_refusals(kw, status, word):
+    assert forward(window(**kw)) == status
+    assert word in LIB.bsa_ops_last_error().decode()
+
+
+def test_window_pointers_and_workspace():
+    s = window()
+    assert forward(None) == INVALID
+    for name in ("q", "k", "v", "o"):
+        assert forward(s, {name: None}) == INVALID and name in LIB.bsa_ops_last_error().decode()
+        assert forward(s, {name: PTR + 8}) == INVALID and "aligned" in LIB.bsa_ops_last_error().decode()
+    need = ctypes.c_size_t()
+    one = window(seq_q=1, seq_kv=5000, left=4000)
+    assert LIB.bsa_window_workspace(ctypes.byref(one), 0, ctypes.byref(need)) == 0 and need.value > 0
+    assert forward(one, ws=None) == INVALID and "workspace" in LIB.bsa_ops_last_error().decode()
+    assert forward(one, n=need.value - 1) == INVALID
+    assert forward(one, ws=PTR + 4) == INVALID
+    assert LIB.bsa_window_workspace(ctypes.byref(one), 0, None) == INVALID
+    assert LIB.bsa_window_workspace(ctypes.byref(window(heads=5)), 0, ctypes.byref(need)) == INVALID and need.value == 0
+
+
+def test_window_backward_refusals():
+    s = window()
+    g = grads(s)
+    assert backward(s, None) == INVALID
+    for name in ("q", "k", "v", "o", "lse", "dout", "dq", "dk", "dv"):
+        assert backward(s, g, {name: None}) == INVALID and name in LIB.bsa_ops_last_error().decode()
+    assert backward(s, g, ws=None) == INVALID and "workspace" in LIB.bsa_ops_last_error().decode()
+    assert backward(s, grads(s, dk_stride=(0, 128, 256))) == INVALID and "overlap" in LIB.bsa_ops_last_error().decode()
+    assert backward(s, grads(s, dq_stride=(100 * 512, 128, 516))) == INVALID
+    assert backward(s, grads(s, do_stride=(0, 128, 1 << 23))) == UNSUPPORTED
+    assert backward(window(q_stride=(0, 128, 1 << 24)), g) == UNSUPPORTED
+
+
+def rope(ptrs=None, positions=None, rows=None, freq=PTR, **kw):
+    s = _ops_ffi.RopeShapes()
+    s.batch, s.heads, s.kv_heads, s.seq, s.head_dim, s.dtype = 2, 4, 2, 30, 64, _ffi.DTYPE_BF16
+    s.pairs, s.grid, s.kv_rows = (16, 8, 8), (2, 3, 5), 30
+    for f, v in kw.items():
+        if not f.endswith("stride"):
+            setattr(s, f, v)
+    s.q_stride = s.q_out_stride = contiguous(30, s.heads, s.head_dim)
+    s.k_stride = s.k_out_stride = s.v_stride = s.v_out_stride = contiguous(30, max(s.kv_heads, 1), s.head_dim)
+    for f, v in kw.items():
+        if f.endswith("stride"):
+            setattr(s, f, v)
+    p = dict(q=PTR, k=PTR, v=PTR, q_out=2 * PTR, k_out=2 * PTR, v_out=2 * PTR)
+    p.update(ptrs or {})
+    return LIB.bsa_rope(ctypes.byref(s), freq, positions, None, rows, p["q"], p["k"], p["v"], p["q_out"], p["k_out"],
+                        p["v_out"], None)
+
+
+BAD_ROPE = [
+    (dict(batch=-1), INVALID, "negative"), (dict(seq=-1), INVALID, "negative"), (dict(heads=0), INVALID, "positive"),
+    (dict(kv_heads=-1), INVALID, "negative"), (dict(kv_rows=-1), INVALID, "negative"),
+    (dict(dtype=5), UNSUPPORTED, "float32"), (dict(head_dim=60), UNSUPPORTED, "head_dim"),
+    (dict(head_dim=264), UNSUPPORTED, "head_dim"), (dict(pairs=(-1, 0, 0)), INVALID, "pairs"),
+    (dict(pairs=(16, 16, 1)), INVALID, "pairs"), (dict(freq=None), INVALID, "freq"),
+    (dict(grid=(0, 1, 1)), INVALID, "grid"), (dict(grid=(1, 1 << 20, 1 << 20)), INVALID, "grid"),
+    (dict(origin=(1 << 30, 0, 0)), INVALID, "positions"), (dict(positions=PTR, pos_stride=(-1, 0)), INVALID, "positions"),
+    (dict(ptrs=dict(q=None)), INVALID, "q"), (dict(ptrs=dict(k=None)), INVALID, "k"),
+    (dict(ptrs=dict(q_out=None)), INVALID, "q_out"), (dict(ptrs=dict(k_out=None)), INVALID, "k_out"),
+    (dict(ptrs=dict(v_out=PTR + 2)), INVALID, "v_out"), (dict(q_stride=(7680, 64, 257)), INVALID, "aligned"),
+    (dict(k_out_stride=(0, 64, 128)), INVALID, "overlap"), (dict(seq=(1 << 29) + 1), UNSUPPORTED, "2^29"),
+    (dict(ptrs=dict(k_out=PTR), rows=PTR), INVALID, "in place"),
+    (dict(ptrs=dict(q_out=PTR), q_out_stride=(7680, 1920, 64)), INVALID, "in place"),
+]
+
+
+@pytest.mark.parametrize("kw,status,word", BAD_ROPE)
+def test_rope_refusals(kw, status, word):
+    assert rope(**kw) == status
+    assert word in LIB.bsa_ops_last_error().decode()
+
+
+def test_binding_refusals_on_the_host():
+    import torch
+    t = torch.zeros((1, 4, 2, 64), dtype=torch.bfloat16)
+    with pytest.raises(TypeError, match="CUDA"):
+        bsa.window_forward(t, t, t, 3)
+    with pytest.raises(TypeError, match="CUDA"):
+        bsa.rope(t, freq=None, pairs=(1,), grid=(1, 1, 4))
+    f = bsa.rope_frequencies((2, 2), theta=16.0, device="cpu")
+    assert f.tolist() == [1.0, 0.25, 1.0, 0.25]
+    assert bsa.rope_frequencies((2, 2), theta=16.0, shared=True, device="cpu").tolist() == [1.0, 0.5, 0.25, 0.125]
