@@ -34,15 +34,21 @@ class WindowGrads(ctypes.Structure):
     _fields_ = [("do_stride", _Stride), ("dq_stride", _Stride), ("dk_stride", _Stride), ("dv_stride", _Stride)]
 
 
-# (name, restype, argtypes) of every exported entry point
+# (name, restype, argtypes) of every exported entry point; the shape structures
+# go by address: byref() of one of the above, or the same bytes
 SIGNATURES = [
     ("bsa_ops_last_error", ctypes.c_char_p, []),
-    ("bsa_rope", c_i32, [ctypes.POINTER(RopeShapes)] + [c_vp] * 11),
-    ("bsa_window_workspace", c_i32, [ctypes.POINTER(WindowShapes), c_i32, ctypes.POINTER(c_sz)]),
-    ("bsa_window_forward", c_i32, [ctypes.POINTER(WindowShapes)] + [c_vp] * 8 + [c_sz, c_vp]),
-    ("bsa_window_backward", c_i32, [ctypes.POINTER(WindowShapes), ctypes.POINTER(WindowGrads)] + [c_vp] * 12 +
-     [c_sz, c_vp]),
+    ("bsa_rope", c_i32, [c_vp] * 12),
+    ("bsa_window_workspace", c_i32, [c_vp, c_i32, ctypes.POINTER(c_sz)]),
+    ("bsa_window_forward", c_i32, [c_vp] * 9 + [c_sz, c_vp]),
+    ("bsa_window_backward", c_i32, [c_vp] * 14 + [c_sz, c_vp]),
 ]
+
+
+# The same layouts for struct.pack (no field is padded).
+ROPE_PACK = "=18i20q"
+WINDOW_PACK = "=10ifi12q"
+GRADS_PACK = "=12q"
 
 
 def load() -> ctypes.CDLL:

@@ -6,21 +6,38 @@ aligned rows.  Work runs on the tensors' device, on its current stream unless
 one is given; outputs and workspaces that are not passed in are allocated for
 that stream.  Nothing here takes part in autograd: backward passes are calls of
 their own (rope with inverse=True, window_backward).
+
+A call of a few microseconds on the device is bound by what the host does for
+it, so the checks take each tensor's properties once, the shape structures are
+packed in one go, and the device is only changed where it differs.  (One token
+of one stream over a cache, two launches: 21 us with a structure filled field by
+field and a device context around every call.)
 """
 from __future__ import annotations
 
 import contextlib
 import ctypes
 import math
+import struct
 from typing import Optional, Sequence, Tuple
 
 from . import _ops_ffi
 from ._ffi import BSA_OK, BsaError, DTYPE_BF16, DTYPE_F16, DTYPE_F32
-from ._ops_ffi import RopeShapes, WindowGrads, WindowShapes
 
 _lib = _ops_ffi.load()
 
+try:
+    import torch
+    _CODES = {torch.bfloat16: DTYPE_BF16, torch.float16: DTYPE_F16, torch.float32: DTYPE_F32}
+except ImportError:  # the package's host functions work without it
+    torch = None
+
 ALL = -1  # window sides: every key
+
+_pack_rope = struct.Struct(_ops_ffi.ROPE_PACK).pack
+_pack_window = struct.Struct(_ops_ffi.WINDOW_PACK).pack
+_pack_grads = struct.Struct(_ops_ffi.GRADS_PACK).pack
+_INT_MAX = (1 << 31) - 1
 
 
 def _check(status: int):
@@ -28,63 +45,62 @@ def _check(status: int):
         raise BsaError(status, _lib.bsa_ops_last_error().decode(errors="replace"))
 
 
-def _torch():
-    import torch
-    return torch
-
-
-def _dtype_code(dtype):
-    torch = _torch()
-    code = {torch.bfloat16: DTYPE_BF16, torch.float16: DTYPE_F16, torch.float32: DTYPE_F32}.get(dtype)
-    if code is None:
-        raise TypeError("tensors must be bfloat16, float16 or float32, not %s" % dtype)
-    return code
-
-
-def _want(name, t, like=None, shape=None):
-    """t as a [B, N, H, d] tensor of like's device and type."""
-    torch = _torch()
+def _first(name, t):
+    """(device, type, type code) of the tensor that the others are held to."""
     if not isinstance(t, torch.Tensor) or not t.is_cuda:
         raise TypeError("%s must be a CUDA tensor" % name)
-    if t.dim() != 4 or (t.shape[3] > 1 and t.stride(3) != 1):
+    dtype = t.dtype
+    code = _CODES.get(dtype)
+    if code is None:
+        raise TypeError("tensors must be bfloat16, float16 or float32, not %s" % dtype)
+    return t.device, dtype, code
+
+
+def _rows(name, t, device, dtype, shape=None):
+    """Strides of t, a [B, N, H, d] tensor of that device, type and (if given)
+    shape, with d contiguous."""
+    if not isinstance(t, torch.Tensor) or t.device != device or t.dtype is not dtype:
+        raise TypeError("%s must be a %s tensor on %s" % (name, dtype, device))
+    s = t.stride()
+    if len(s) != 4 or (s[3] != 1 and t.shape[3] > 1):
         raise ValueError("%s must be [B, N, H, d] with d contiguous" % name)
-    if like is not None and (t.dtype != like.dtype or t.device != like.device):
-        raise TypeError("%s must be %s on %s" % (name, like.dtype, like.device))
-    if shape is not None and tuple(t.shape) != tuple(shape):
+    if shape is not None and t.shape != shape:
         raise ValueError("%s must have shape %s, not %s" % (name, tuple(shape), tuple(t.shape)))
-    return t
+    return s
 
 
-def _want_ints(name, t, device, shape):
-    torch = _torch()
+def _ints(name, t, device, n):
+    """Address of t, int32 [n] on the device (None: NULL)."""
     if t is None:
         return None
-    if not isinstance(t, torch.Tensor) or t.dtype != torch.int32 or t.device != device:
+    if not isinstance(t, torch.Tensor) or t.dtype is not torch.int32 or t.device != device:
         raise TypeError("%s must be an int32 tensor on %s" % (name, device))
-    if tuple(t.shape) != tuple(shape) or (t.numel() > 1 and t.stride(-1) != 1):
-        raise ValueError("%s must have shape %s, its last dimension contiguous" % (name, tuple(shape)))
+    if t.shape != (n,) or (n > 1 and t.stride(0) != 1):
+        raise ValueError("%s must be contiguous and have shape (%d,)" % (name, n))
     return t.data_ptr()
-
-
-def _set(dst, t):
-    s = t.stride()
-    dst[0], dst[1], dst[2] = s[0], s[2], s[1]
 
 
 @contextlib.contextmanager
 def _on(device, stream):
-    """Makes `device` current, and yields the handle of `stream` (None: the
-    device's current stream); allocations inside belong to that stream."""
-    torch = _torch()
+    """Makes `device` and `stream` (None: the device's current one) current, so
+    that allocations belong to them, and yields the stream's handle."""
     with torch.cuda.device(device):
         if stream is None:
-            yield torch.cuda.current_stream(device).cuda_stream
+            yield torch.cuda.current_stream().cuda_stream
             return
         handle = stream.cuda_stream if hasattr(stream, "cuda_stream") else int(stream)
         if not hasattr(stream, "cuda_stream"):
             stream = torch.cuda.ExternalStream(handle, device=device) if handle else torch.cuda.default_stream(device)
         with torch.cuda.stream(stream):
             yield handle
+
+
+def _run(device, stream, call):
+    """call(handle) with `device` and `stream` current."""
+    if stream is None and torch.cuda.current_device() == device.index:
+        return call(torch.cuda.current_stream().cuda_stream)
+    with _on(device, stream) as handle:
+        return call(handle)
 
 
 # ----------------------------------------------------------------------------
@@ -94,12 +110,14 @@ def rope_frequencies(pairs: Sequence[int], theta: float = 10000.0, shared: bool 
     """float64 [sum(pairs)] angles per position, for `pairs` turned pairs on each
     axis: theta^(-i / n) over the n pairs of each axis, or with shared=True over
     all pairs in a row (text and image positions that share one ladder)."""
-    torch = _torch()
     n_all, f = sum(pairs), []
     for n in pairs:
         start = len(f)
         f += [theta ** (-((start + i) / n_all if shared else i / n)) for i in range(n)]
     return torch.tensor(f, dtype=torch.float64, device=device)
+
+
+_NO_STRIDE = (0, 0, 0, 0)
 
 
 def rope(q, k=None, v=None, *, freq, pairs: Sequence[int], interleaved: bool = True, positions=None,
@@ -117,135 +135,120 @@ def rope(q, k=None, v=None, *, freq, pairs: Sequence[int], interleaved: bool = T
     sequences' first tokens go to (new tokens of a cache [B, capacity, Hkv, d]);
     v is copied there unturned.  inverse=True turns back: the backward pass on
     gradients.  out_q may be q, and out_k k.  Returns the outputs of the tensors
-    given, allocated where they are not passed in."""
-    torch = _torch()
-    _want("q", q)
-    B, N, H, d = q.shape
-    s = RopeShapes()
-    s.dtype = _dtype_code(q.dtype)
-    dev = q.device
-    if v is not None and k is None:
-        raise ValueError("v needs k")
-    Hkv = 0
+    given, allocated where they are not passed in (zeros behind `lengths`)."""
+    dev, dtype, code = _first("q", q)
+    qs = _rows("q", q, dev, dtype)
+    B, N, H, d = q_shape = q.shape
+    Hkv, ks, vs = 0, _NO_STRIDE, _NO_STRIDE
     if k is not None:
-        _want("k", k, q)
-        Hkv = k.shape[2]
-        if tuple(k.shape) != (B, N, Hkv, d):
-            raise ValueError("k must have shape %s, not %s" % ((B, N, Hkv, d), tuple(k.shape)))
+        Hkv = k.shape[2] if k.dim() == 4 else 0
+        kv_shape = (B, N, Hkv, d)
+        ks = _rows("k", k, dev, dtype, kv_shape)
         if v is not None:
-            _want("v", v, q, k.shape)
-    pairs = tuple(int(x) for x in pairs)
-    if not 1 <= len(pairs) <= 3:
+            vs = _rows("v", v, dev, dtype, kv_shape)
+    elif v is not None or rows is not None:
+        raise ValueError("v and rows need k")
+    n_axes = len(pairs)
+    if not 1 <= n_axes <= 3:
         raise ValueError("pairs must name one to three axes")
-    if (not isinstance(freq, torch.Tensor) or freq.dtype != torch.float64 or freq.device != dev or
-            tuple(freq.shape) != (sum(pairs),) or not freq.is_contiguous()):
+    p0, p1, p2 = (tuple(pairs) + (0, 0))[:3]
+    if (not isinstance(freq, torch.Tensor) or freq.dtype is not torch.float64 or freq.device != dev or
+            freq.shape != (p0 + p1 + p2,) or not freq.is_contiguous()):
         raise TypeError("freq must be a contiguous float64 tensor of sum(pairs) elements on %s" % dev)
-    if (positions is None) == (grid is None):
-        raise ValueError("give either positions or grid")
-    if rows is not None and k is None:
-        raise ValueError("rows needs k")
-    pos_ptr = None
+    g0 = g1 = g2 = o0 = o1 = o2 = 0
+    pos_ptr, ps0, ps1 = None, 0, 0
     if positions is not None:
-        if not isinstance(positions, torch.Tensor) or positions.dim() != 3:
-            raise TypeError("positions must be an int32 tensor [axes, B, N]")
-        if positions.shape[0] < len(pairs) or positions.shape[1] not in (1, B):
-            raise ValueError("positions must be [axes, B, N] or [axes, 1, N] with at least %d axes" % len(pairs))
-        pos_ptr = _want_ints("positions", positions, dev, (positions.shape[0], positions.shape[1], N))
-        s.pos_stride[0] = positions.stride(0)
-        s.pos_stride[1] = positions.stride(1) if positions.shape[1] == B and B > 1 else 0
+        if grid is not None:
+            raise ValueError("give either positions or grid")
+        if not isinstance(positions, torch.Tensor) or positions.dtype is not torch.int32 or positions.device != dev:
+            raise TypeError("positions must be an int32 tensor on %s" % dev)
+        shape = positions.shape
+        if len(shape) != 3 or shape[0] < n_axes or shape[1] not in (1, B) or shape[2] != N:
+            raise ValueError("positions must be [axes, B, N] or [axes, 1, N] with at least %d axes" % n_axes)
+        ps0, ps1, ps2 = positions.stride()
+        if N > 1 and ps2 != 1:
+            raise ValueError("positions must be contiguous along the tokens")
+        if shape[1] == 1:
+            ps1 = 0
+        pos_ptr = positions.data_ptr()
+    elif grid is None:
+        raise ValueError("give either positions or grid")
     else:
-        if len(grid) != 3 or len(origin) != 3:
-            raise ValueError("grid and origin must be (time, height, width)")
-        for i in range(3):
-            s.grid[i], s.origin[i] = int(grid[i]), int(origin[i])
-    len_ptr = _want_ints("lengths", lengths, dev, (B,))
-    row_ptr = _want_ints("rows", rows, dev, (B,))
+        (g0, g1, g2), (o0, o1, o2) = grid, origin
+    len_ptr, row_ptr = _ints("lengths", lengths, dev, B), _ints("rows", rows, dev, B)
     if rows is not None and (out_k is None or (v is not None and out_v is None)):
         raise ValueError("rows needs the caches as out_k (and out_v)")
-    for i, n in enumerate(pairs):
-        s.pairs[i] = n
-    s.batch, s.heads, s.kv_heads, s.seq, s.head_dim = B, H, Hkv, N, d
-    s.interleaved, s.inverse = 1 if interleaved else 0, 1 if inverse else 0
-    with _on(dev, stream) as handle:
+
+    def call(handle):
+        nonlocal out_q, out_k, out_v
         # (rows behind a sequence's end are not written: zeros there, not stale memory)
-        new = torch.zeros_like if lengths is not None else torch.empty_like
-        fresh = lambda t: new(t, memory_format=torch.contiguous_format)
-        out_q = fresh(q) if out_q is None else _want("out_q", out_q, q, q.shape)
-        _set(s.q_stride, q)
-        _set(s.q_out_stride, out_q)
-        outs = [out_q]
+        new = torch.empty if lengths is None else torch.zeros
+        if out_q is None:
+            out_q = new(q_shape, dtype=dtype, device=dev)
+        oqs, oks, ovs, cap = _rows("out_q", out_q, dev, dtype, q_shape), _NO_STRIDE, _NO_STRIDE, 0
         if k is not None:
             if out_k is None:
-                out_k = fresh(k)
-            _want("out_k", out_k, q)
-            cap = out_k.shape[1]
-            if tuple(out_k.shape) != (B, cap, Hkv, d) or (rows is None and cap < N):
-                raise ValueError("out_k must be [%d, %s, %d, %d]" % (B, "tokens" if rows is not None else N, Hkv, d))
-            s.kv_rows = cap
-            _set(s.k_stride, k)
-            _set(s.k_out_stride, out_k)
-            outs.append(out_k)
+                out_k = new(kv_shape, dtype=dtype, device=dev)
+            if v is not None and out_v is None:
+                out_v = new(kv_shape, dtype=dtype, device=dev)
+            cap = N if rows is None else out_k.shape[1] if out_k.dim() == 4 else 0
+            out_shape = (B, cap, Hkv, d)
+            oks = _rows("out_k", out_k, dev, dtype, out_shape)
             if v is not None:
-                out_v = fresh(v) if out_v is None else out_v
-                _want("out_v", out_v, q)
-                if tuple(out_v.shape[::2]) != (B, Hkv) or out_v.shape[3] != d or out_v.shape[1] < (
-                        cap if rows is not None else N):
-                    raise ValueError("out_v must be shaped like out_k")
-                s.kv_rows = min(cap, out_v.shape[1])
-                _set(s.v_stride, v)
-                _set(s.v_out_stride, out_v)
-                outs.append(out_v)
-        _check(_lib.bsa_rope(ctypes.byref(s), freq.data_ptr(), pos_ptr, len_ptr, row_ptr, q.data_ptr(),
+                ovs = _rows("out_v", out_v, dev, dtype, out_shape)
+        s = _pack_rope(B, H, Hkv, N, d, code, p0, p1, p2, 1 if interleaved else 0, 1 if inverse else 0, g0, g1, g2, o0,
+                       o1, o2, cap, ps0, ps1, qs[0], qs[2], qs[1], ks[0], ks[2], ks[1], vs[0], vs[2], vs[1],
+                       oqs[0], oqs[2], oqs[1], oks[0], oks[2], oks[1], ovs[0], ovs[2], ovs[1])
+        _check(_lib.bsa_rope(s, freq.data_ptr(), pos_ptr, len_ptr, row_ptr, q.data_ptr(),
                              None if k is None else k.data_ptr(), None if v is None else v.data_ptr(),
                              out_q.data_ptr(), None if k is None else out_k.data_ptr(),
                              None if v is None else out_v.data_ptr(), handle))
-    return tuple(outs)
+
+    _run(dev, stream, call)
+    return (out_q,) if k is None else (out_q, out_k) if v is None else (out_q, out_k, out_v)
 
 
 # ----------------------------------------------------------------------------
 # Window attention
 
-def _window_shapes(q, k, v, left, right, sinks, scale):
-    _want("q", q)
-    _want("k", k, q)
-    _want("v", v, q)
-    B, Nq, H, d = q.shape
-    Nkv, Hkv = k.shape[1], k.shape[2]
-    if tuple(k.shape) != (B, Nkv, Hkv, d) or tuple(v.shape) != (B, Nkv, Hkv, d):
-        raise ValueError("inconsistent q/k/v shapes")
-    s = WindowShapes()
-    s.batch, s.heads, s.kv_heads, s.seq_q, s.seq_kv, s.head_dim = B, H, Hkv, Nq, Nkv, d
-    s.dtype = _dtype_code(q.dtype)
-    big = (1 << 31) - 1
-    s.left, s.right, s.sinks = min(int(left), big), min(int(right), big), min(int(sinks), big)
-    if scale is not None and not (scale > 0 and math.isfinite(scale)):
+def _window_head(q, k, v, left, right, sinks, scale):
+    """(device, type, q's shape, k's shape, packed fields but O's strides)"""
+    dev, dtype, code = _first("q", q)
+    qs = _rows("q", q, dev, dtype)
+    B, Nq, H, d = q_shape = q.shape
+    ks = _rows("k", k, dev, dtype)
+    k_shape = k.shape
+    _, Nkv, Hkv, _ = k_shape
+    if k_shape[0] != B or k_shape[3] != d:
+        raise ValueError("inconsistent q/k shapes")
+    vs = _rows("v", v, dev, dtype, k_shape)
+    if scale is None:
+        scale = 0.0
+    elif not (scale > 0 and math.isfinite(scale)):
         raise ValueError("scale must be positive and finite")
-    s.scale = 0.0 if scale is None else scale
-    _set(s.q_stride, q)
-    _set(s.k_stride, k)
-    _set(s.v_stride, v)
-    return s
+    fields = (B, H, Hkv, Nq, Nkv, d, code, min(left, _INT_MAX), min(right, _INT_MAX), min(sinks, _INT_MAX), scale, 0,
+              qs[0], qs[2], qs[1], ks[0], ks[2], ks[1], vs[0], vs[2], vs[1])
+    return dev, dtype, q_shape, k_shape, fields
 
 
-def _lse_of(lse, q):
-    torch = _torch()
-    B, Nq, H, _ = q.shape
-    if (not isinstance(lse, torch.Tensor) or lse.dtype != torch.float32 or lse.device != q.device or
-            tuple(lse.shape) != (B, H, Nq) or not lse.is_contiguous()):
-        raise TypeError("lse must be a contiguous float32 tensor [B, H, Nq] on %s" % q.device)
+def _lse_of(lse, dev, shape):
+    if (not isinstance(lse, torch.Tensor) or lse.dtype is not torch.float32 or lse.device != dev or
+            lse.shape != shape or not lse.is_contiguous()):
+        raise TypeError("lse must be a contiguous float32 tensor of shape %s on %s" % (shape, dev))
     return lse
 
 
 def _workspace(s, backward, workspace, device):
-    """(pointer, bytes, tensor to keep alive until the call is made)"""
-    torch = _torch()
+    """(address, bytes, the tensor)"""
     need = ctypes.c_size_t()
-    _check(_lib.bsa_window_workspace(ctypes.byref(s), backward, ctypes.byref(need)))
-    if need.value == 0:
+    _check(_lib.bsa_window_workspace(s, backward, ctypes.byref(need)))
+    n = need.value
+    if n == 0:
         return None, 0, None
     if workspace is None:
-        workspace = torch.empty(need.value, dtype=torch.uint8, device=device)
-    elif workspace.device != device or not workspace.is_contiguous():
+        workspace = torch.empty(n, dtype=torch.uint8, device=device)
+        return workspace.data_ptr(), n, workspace
+    if not isinstance(workspace, torch.Tensor) or workspace.device != device or not workspace.is_contiguous():
         raise TypeError("workspace must be a contiguous tensor on %s" % device)
     return workspace.data_ptr(), workspace.numel() * workspace.element_size(), workspace
 
@@ -254,9 +257,8 @@ def window_workspace(q, k, v, left: int, right: int = 0, sinks: int = 0, *, back
     """Bytes of device workspace that window_forward or window_backward needs for
     these tensors, for callers that pass their own."""
     need = ctypes.c_size_t()
-    s = _window_shapes(q, k, v, left, right, sinks, None)
-    _set(s.o_stride, q)
-    _check(_lib.bsa_window_workspace(ctypes.byref(s), 1 if backward else 0, ctypes.byref(need)))
+    fields = _window_head(q, k, v, left, right, sinks, None)[4]
+    _check(_lib.bsa_window_workspace(_pack_window(*fields, 0, 0, 0), 1 if backward else 0, ctypes.byref(need)))
     return need.value
 
 
@@ -271,24 +273,24 @@ def window_forward(q, k, v, left: int, right: int = 0, sinks: int = 0, *, scale:
     the device (default: Nq, Nkv).  Returns (o, lse), lse float32 [B, H, Nq]; a
     query that sees nothing gets o = 0 and lse = -inf.  Rows of a given o and
     lse from q_len on keep what they held; allocated ones hold zeros there."""
-    torch = _torch()
-    s = _window_shapes(q, k, v, left, right, sinks, scale)
-    B, Nq, H, _ = q.shape
-    dev = q.device
-    ql, kl = _want_ints("q_len", q_len, dev, (B,)), _want_ints("kv_len", kv_len, dev, (B,))
-    with _on(dev, stream) as handle:
+    dev, dtype, q_shape, _, fields = _window_head(q, k, v, left, right, sinks, scale)
+    B, Nq, H, _ = q_shape
+    ql, kl = _ints("q_len", q_len, dev, B), _ints("kv_len", kv_len, dev, B)
+
+    def call(handle):
+        nonlocal o, lse
+        new = torch.empty if q_len is None else torch.zeros
         if o is None:
-            o = (torch.empty if q_len is None else torch.zeros)(q.shape, dtype=q.dtype, device=dev)
-        else:
-            _want("o", o, q, q.shape)
+            o = new(q_shape, dtype=dtype, device=dev)
         if lse is None:
-            lse = (torch.empty if q_len is None else torch.zeros)((B, H, Nq), dtype=torch.float32, device=dev)
-        else:
-            _lse_of(lse, q)
-        _set(s.o_stride, o)
-        ws, n, keep = _workspace(s, 0, workspace, dev)
-        _check(_lib.bsa_window_forward(ctypes.byref(s), q.data_ptr(), k.data_ptr(), v.data_ptr(), o.data_ptr(),
-                                       lse.data_ptr(), ql, kl, ws, n, handle))
+            lse = new((B, H, Nq), dtype=torch.float32, device=dev)
+        os, _ = _rows("o", o, dev, dtype, q_shape), _lse_of(lse, dev, (B, H, Nq))
+        s = _pack_window(*fields, os[0], os[2], os[1])
+        ws, n, _keep = _workspace(s, 0, workspace, dev)
+        _check(_lib.bsa_window_forward(s, q.data_ptr(), k.data_ptr(), v.data_ptr(), o.data_ptr(), lse.data_ptr(), ql,
+                                       kl, ws, n, handle))
+
+    _run(dev, stream, call)
     return o, lse
 
 
@@ -298,28 +300,29 @@ def window_backward(q, k, v, o, lse, do, left: int, right: int = 0, sinks: int =
     (bsa_window_backward), with the o and lse that it returned and its other
     arguments unchanged.  Rows of given dq from q_len on, and of dk and dv from
     kv_len on, keep what they held; allocated ones hold zeros there."""
-    torch = _torch()
-    s = _window_shapes(q, k, v, left, right, sinks, scale)
-    B, Nq, H, _ = q.shape
-    dev = q.device
-    _want("o", o, q, q.shape)
-    _want("do", do, q, q.shape)
-    _lse_of(lse, q)
-    ql, kl = _want_ints("q_len", q_len, dev, (B,)), _want_ints("kv_len", kv_len, dev, (B,))
-    g = WindowGrads()
-    with _on(dev, stream) as handle:
-        def grad(name, t, x, ragged):
-            if t is None:
-                return (torch.empty if ragged is None else torch.zeros)(x.shape, dtype=x.dtype, device=dev)
-            return _want(name, t, x, x.shape)
-        dq, dk, dv = grad("dq", dq, q, q_len), grad("dk", dk, k, kv_len), grad("dv", dv, v, kv_len)
-        _set(s.o_stride, o)
-        _set(g.do_stride, do)
-        _set(g.dq_stride, dq)
-        _set(g.dk_stride, dk)
-        _set(g.dv_stride, dv)
-        ws, n, keep = _workspace(s, 1, workspace, dev)
-        _check(_lib.bsa_window_backward(ctypes.byref(s), ctypes.byref(g), q.data_ptr(), k.data_ptr(), v.data_ptr(),
-                                        o.data_ptr(), lse.data_ptr(), do.data_ptr(), dq.data_ptr(), dk.data_ptr(),
-                                        dv.data_ptr(), ql, kl, ws, n, handle))
+    dev, dtype, q_shape, k_shape, fields = _window_head(q, k, v, left, right, sinks, scale)
+    B, Nq, H, _ = q_shape
+    os, gs = _rows("o", o, dev, dtype, q_shape), _rows("do", do, dev, dtype, q_shape)
+    _lse_of(lse, dev, (B, H, Nq))
+    ql, kl = _ints("q_len", q_len, dev, B), _ints("kv_len", kv_len, dev, B)
+
+    def call(handle):
+        nonlocal dq, dk, dv
+        if dq is None:
+            dq = (torch.empty if q_len is None else torch.zeros)(q_shape, dtype=dtype, device=dev)
+        new = torch.empty if kv_len is None else torch.zeros
+        if dk is None:
+            dk = new(k_shape, dtype=dtype, device=dev)
+        if dv is None:
+            dv = new(k_shape, dtype=dtype, device=dev)
+        dqs = _rows("dq", dq, dev, dtype, q_shape)
+        dks, dvs = _rows("dk", dk, dev, dtype, k_shape), _rows("dv", dv, dev, dtype, k_shape)
+        s = _pack_window(*fields, os[0], os[2], os[1])
+        g = _pack_grads(gs[0], gs[2], gs[1], dqs[0], dqs[2], dqs[1], dks[0], dks[2], dks[1], dvs[0], dvs[2], dvs[1])
+        ws, n, _keep = _workspace(s, 1, workspace, dev)
+        _check(_lib.bsa_window_backward(s, g, q.data_ptr(), k.data_ptr(), v.data_ptr(), o.data_ptr(), lse.data_ptr(),
+                                        do.data_ptr(), dq.data_ptr(), dk.data_ptr(), dv.data_ptr(), ql, kl, ws, n,
+                                        handle))
+
+    _run(dev, stream, call)
     return dq, dk, dv

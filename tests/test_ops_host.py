@@ -48,6 +48,25 @@ def test_ctypes_layout_matches_the_header(tmp_path):
             assert got[(c, f)] == getattr(cls, f).offset, (c, f)
 
 
+def test_packed_layouts_are_the_structures():
+    import struct
+    for cls, fmt in ((_ops_ffi.RopeShapes, _ops_ffi.ROPE_PACK), (_ops_ffi.WindowShapes, _ops_ffi.WINDOW_PACK),
+                     (_ops_ffi.WindowGrads, _ops_ffi.GRADS_PACK)):
+        assert struct.calcsize(fmt) == ctypes.sizeof(cls)
+        flat, values = [], []
+        for f, ct in cls._fields_:
+            n = ct._length_ if hasattr(ct, "_length_") else 1
+            flat.append((f, n))
+        n_all = sum(n for _, n in flat)
+        values = [(float(i) if cls is _ops_ffi.WindowShapes and i == 10 else i) for i in range(n_all)]
+        got = cls.from_buffer_copy(struct.pack(fmt, *values))
+        at = 0
+        for f, n in flat:
+            v = getattr(got, f)
+            assert (list(v) if n > 1 else [v]) == values[at:at + n], f
+            at += n
+
+
 def test_build_options():
     b = _builder()
     for src in b.OPS_SOURCES:
