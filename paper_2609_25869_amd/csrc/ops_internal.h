@@ -62,8 +62,21 @@ struct WindowArgs {
   Strides dos, dqs, dks, dvs;
   float* stats;        // [B, H, 2, stat_rows]: base-2 LSE, and row sums of dO * O
   int64_t stat_rows;   // at least Nq + 31: whole tiles of rows may be read
-  int32_t nktiles;     // key tiles per key head
+  // dK/dV: key tiles per key head, those that hold sinks (the first ones), and the
+  // slices that the queries of a tile with and without sinks are cut into
+  int32_t nktiles, nsink, sink_slices, slices;
 };
+
+// Key tiles of one key head as work items of the dK/dV kernel: the slices of the
+// tiles with sinks, then those of the others.  A tile cut into several slices has
+// partial sums in the workspace, in the order of the items.
+inline __host__ __device__ int64_t dkv_items(const WindowArgs& a) {
+  return (int64_t)a.nsink * a.sink_slices + (int64_t)(a.nktiles - a.nsink) * a.slices;
+}
+inline __host__ __device__ int64_t dkv_parts(const WindowArgs& a) {
+  return (a.sink_slices > 1 ? (int64_t)a.nsink * a.sink_slices : 0) +
+         (a.slices > 1 ? (int64_t)(a.nktiles - a.nsink) * a.slices : 0);
+}
 
 constexpr int32_t kFar = 1 << 30;
 
@@ -76,10 +89,8 @@ struct ForwardPlan {
   int64_t part_floats;  // of the workspace
 };
 ForwardPlan plan_forward(const WindowArgs& a, int d);
-struct BackwardPlan {
-  int32_t ntiles, nktiles;
-  int64_t stat_rows, floats;  // floats: of the workspace
-};
-BackwardPlan plan_backward(const WindowArgs& a, int d);
+// Sets the backward pass's tile counts, slices and stat_rows; returns the floats of
+// its workspace (stats, then partial sums).
+int64_t plan_backward(WindowArgs* a, int d);
 
 }  // namespace bsa_ops

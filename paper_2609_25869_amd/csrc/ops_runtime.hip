@@ -118,8 +118,8 @@ WindowArgs window_args(const bsa_window_shapes& s) {
   return a;
 }
 
-int64_t window_bytes(const WindowArgs& a, int d, bool backward) {
-  return 4 * (backward ? plan_backward(a, d).floats : plan_forward(a, d).part_floats);
+int64_t window_bytes(WindowArgs a, int d, bool backward) {
+  return 4 * (backward ? plan_backward(&a, d) : plan_forward(a, d).part_floats);
 }
 
 bsa_status check_workspace(int64_t need, const void* workspace, size_t bytes) {

@@ -4,6 +4,10 @@
 //         probabilities again from the scores and the LSE, and also leaves every
 //         row's D = sum(dO o O) and base-2 LSE in the workspace;
 //   dK/dV walks, for 128 keys, the queries that see any of them, head by head.
+//         Sinks are seen by every later query: a tile with sinks is cut into
+//         slices of its queries, of about the length of the other tiles' walks,
+//         and a third kernel adds the slices' sums up in order.  (8192 queries, 16
+//         heads over 4 key heads, window 1024, 4 sinks: 1626 us in one piece.)
 //
 //   P = exp(S - LSE), dS = P o (dO V^T - D)
 //   dQ = scale dS K, dV = P^T dO, dK = scale dS^T Q
@@ -192,8 +196,12 @@ __global__ __launch_bounds__(64 * kWaves) void window_dkv_kernel(WindowArgs a) {
   __shared__ __attribute__((aligned(1024))) uint8_t ring3[kSlot];
   auto slot = [&](int i) -> uint8_t* { return i == 0 ? ring0 : i == 1 ? ring1 : i == 2 ? ring2 : ring3; };
 
-  const int64_t item = item_of_slot(blockIdx.x, (int64_t)a.nktiles * a.B * a.Hkv);
-  const int tile = (int)(item % a.nktiles), bh = (int)(item / a.nktiles);
+  const int64_t items = dkv_items(a), item = item_of_slot(blockIdx.x, items * a.B * a.Hkv);
+  const int bh = (int)(item / items), in_head = (int)(item % items);
+  const bool sink = in_head < a.nsink * a.sink_slices;
+  const int nslice = sink ? a.sink_slices : a.slices;
+  const int in_kind = sink ? in_head : in_head - a.nsink * a.sink_slices;
+  const int tile = in_kind / nslice + (sink ? 0 : a.nsink), slice = in_kind % nslice;
   const int b = bh / a.Hkv, kvh = bh % a.Hkv;
   const Seq sq(a, b);
   const int k0 = tile * TKEY;
@@ -203,7 +211,9 @@ __global__ __launch_bounds__(64 * kWaves) void window_dkv_kernel(WindowArgs a) {
   const int i_lo = seen.first(k0);
   const int i_hi = k0 < a.sinks ? sq.q_len - 1 : seen.last(min(k0 + TKEY, sq.kv_len) - 1);
   const int per_head = max(i_hi - i_lo + TR, 0) / TR;  // row tiles
-  const int nt = per_head * a.group;
+  const int64_t all = (int64_t)per_head * a.group;
+  const int64_t t_begin = all * slice / nslice;
+  const int nt = (int)(all * (slice + 1) / nslice - t_begin);
 
   const int tid = threadIdx.x, lane = tid & 63;
   const int w = __builtin_amdgcn_readfirstlane(tid >> 6);
@@ -228,7 +238,8 @@ __global__ __launch_bounds__(64 * kWaves) void window_dkv_kernel(WindowArgs a) {
   lq.init(a.qs.n, w, lane);
   ld.init(a.dos.n, w, lane);
   // the row tile that is loaded next, and the one that is worked on
-  int g_in = 0, i_in = i_lo, i_now = i_lo;
+  int g_in = per_head ? (int)(t_begin / per_head) : 0, i_in = i_lo + (per_head ? (int)(t_begin % per_head) : 0) * TR;
+  int i_now = i_in;
   const uint32_t stat_off = (uint32_t)(n * 4) + (hh ? (uint32_t)(a.stat_rows * 4) : 0u);
   auto issue = [&](uint8_t* s) {
     const bool any = g_in < a.group;
@@ -329,6 +340,22 @@ __global__ __launch_bounds__(64 * kWaves) void window_dkv_kernel(WindowArgs a) {
   }
   wait_vm_lgkm<0>();
   if (!live) return;
+  if (nslice > 1) {
+    // [slice][dK, dV][key][column]
+    const int64_t first_part = sink || a.sink_slices == 1 ? 0 : (int64_t)a.nsink * a.sink_slices;
+    float* part = a.part + ((int64_t)bh * dkv_parts(a) + first_part + in_kind) * (2 * TKEY * D) + (key - k0) * D;
+#pragma unroll
+    for (int d = 0; d < R::kBlocks; ++d) {
+#pragma unroll
+      for (int g = 0; g < 4; ++g) {
+        const int c = d * 32 + 8 * g + 4 * hh;
+        *reinterpret_cast<f32x4*>(part + c) = f32x4{dk[d][4 * g], dk[d][4 * g + 1], dk[d][4 * g + 2], dk[d][4 * g + 3]};
+        *reinterpret_cast<f32x4*>(part + TKEY * D + c) =
+            f32x4{dv[d][4 * g], dv[d][4 * g + 1], dv[d][4 * g + 2], dv[d][4 * g + 3]};
+      }
+    }
+    return;
+  }
   T* kp = static_cast<T*>(a.dk) + b * a.dks.b + kvh * a.dks.h + key * a.dks.n;
   T* vp = static_cast<T*>(a.dv) + b * a.dvs.b + kvh * a.dvs.h + key * a.dvs.n;
 #pragma unroll
@@ -347,40 +374,80 @@ __global__ __launch_bounds__(64 * kWaves) void window_dkv_kernel(WindowArgs a) {
 #endif
 }
 
+// Adds up the slices of the key tiles that are cut: one workgroup per 128 x 128
+// columns of dK or dV and tile, four columns a thread.
+template <typename T, int D>
+__global__ __launch_bounds__(256) void window_dkv_sum_kernel(WindowArgs a) {
+  constexpr int TKEY = 32 * kWaves;
+  const int cut_sinks = a.sink_slices > 1 ? a.nsink : 0, cut = cut_sinks + (a.slices > 1 ? a.nktiles - a.nsink : 0);
+  const int bh = blockIdx.x / cut, c = blockIdx.x % cut;
+  const bool sink = c < cut_sinks;
+  const int tile = sink ? c : c - cut_sinks + a.nsink, nslice = sink ? a.sink_slices : a.slices;
+  const int b = bh / a.Hkv, kvh = bh % a.Hkv;
+  const Seq sq(a, b);
+  const int at = ((int)blockIdx.y * 256 + (int)threadIdx.x) * 4;  // in the tile's [key][column]
+  const int key = tile * TKEY + at / D, col = at % D;
+  if (key >= sq.kv_len) return;
+  const int64_t p0 = sink ? (int64_t)c * a.sink_slices
+                          : (int64_t)cut_sinks * a.sink_slices + (int64_t)(c - cut_sinks) * a.slices;
+  const float* part = a.part + ((int64_t)bh * dkv_parts(a) + p0) * (2 * TKEY * D) + blockIdx.z * (TKEY * D) + at;
+  f32x4 sum = {0.f, 0.f, 0.f, 0.f};
+  for (int s = 0; s < nslice; ++s) sum += *reinterpret_cast<const f32x4*>(part + (int64_t)s * (2 * TKEY * D));
+  const float f = blockIdx.z == 0 ? a.scale : 1.f;
+  const Strides& st = blockIdx.z == 0 ? a.dks : a.dvs;
+  T* out = static_cast<T*>(blockIdx.z == 0 ? a.dk : a.dv) + b * st.b + kvh * st.h + key * st.n + col;
+  *reinterpret_cast<u32x2*>(out) = u32x2{pack2<T>(sum[0] * f, sum[1] * f), pack2<T>(sum[2] * f, sum[3] * f)};
+}
+
 template <typename T, int D>
 hipError_t launch(const WindowArgs& a, hipStream_t s) {
-  const int64_t nq = (int64_t)a.ntiles * a.B * a.Hkv, nk = (int64_t)a.nktiles * a.B * a.Hkv;
+  const int64_t bh = (int64_t)a.B * a.Hkv, nq = a.ntiles * bh, nk = dkv_items(a) * bh;
   if (nq > 0x7fffffff || nk > 0x7fffffff) return hipErrorInvalidValue;
   if (nq > 0) {
     hipLaunchKernelGGL((window_dq_kernel<T, D>), dim3((unsigned)nq), dim3(64 * kWaves), 0, s, a);
     const hipError_t e = hipGetLastError();
     if (e != hipSuccess) return e;
   }
-  if (nk > 0) {
-    hipLaunchKernelGGL((window_dkv_kernel<T, D>), dim3((unsigned)nk), dim3(64 * kWaves), 0, s, a);
-    return hipGetLastError();
-  }
-  return hipSuccess;
+  if (nk == 0) return hipSuccess;
+  hipLaunchKernelGGL((window_dkv_kernel<T, D>), dim3((unsigned)nk), dim3(64 * kWaves), 0, s, a);
+  hipError_t e = hipGetLastError();
+  const int64_t cut = (a.sink_slices > 1 ? a.nsink : 0) + (a.slices > 1 ? a.nktiles - a.nsink : 0);
+  if (e != hipSuccess || cut == 0) return e;
+  hipLaunchKernelGGL((window_dkv_sum_kernel<T, D>), dim3((unsigned)(cut * bh), 32 * kWaves * D / 1024, 2), dim3(256), 0, s, a);
+  return hipGetLastError();
 }
 
 }  // namespace
 
-BackwardPlan plan_backward(const WindowArgs& a, int) {
-  BackwardPlan p{};
-  const int64_t rows = (int64_t)a.Nq * a.group;
-  p.ntiles = (int32_t)((rows + 32 * kWaves - 1) / (32 * kWaves));
-  p.nktiles = (a.Nkv + 32 * kWaves - 1) / (32 * kWaves);
-  p.stat_rows = ((int64_t)a.Nq + 63) / 32 * 32;
-  p.floats = (int64_t)a.B * a.H * 2 * p.stat_rows + 32;
-  return p;
+int64_t plan_backward(WindowArgs* a, int d) {
+  constexpr int kKeys = 32 * kWaves;
+  const int64_t rows = (int64_t)a->Nq * a->group;
+  a->ntiles = (int32_t)((rows + 32 * kWaves - 1) / (32 * kWaves));
+  a->nktiles = (a->Nkv + kKeys - 1) / kKeys;
+  a->stat_rows = ((int64_t)a->Nq + 63) / 32 * 32;
+  // Row tiles that a key tile walks.  Every query that lies behind a tile may see
+  // its sinks; others are seen from `right` before to `left` behind.
+  auto min64 = [](int64_t x, int64_t y) { return x < y ? x : y; };
+  auto max64 = [](int64_t x, int64_t y) { return x > y ? x : y; };
+  const int64_t walk_sink = ((int64_t)a->Nq + 31) / 32 * a->group;
+  const int64_t walk = min64(walk_sink, ((int64_t)a->left + a->right + kKeys + 31) / 32 * a->group);
+  a->nsink = (int32_t)((a->sinks + kKeys - 1) / kKeys);
+  // Slices: a tile with sinks is cut to about the others' walk.  Where all that
+  // gives fewer than 512 workgroups, every tile is cut further; no slice is
+  // shorter than eight row tiles.
+  const int64_t bh = max64((int64_t)a->B * a->Hkv, 1);
+  int64_t goal = max64(walk, 8);
+  const int64_t total = bh * (a->nsink * walk_sink + (a->nktiles - a->nsink) * walk);
+  goal = max64(min64(goal, total / 512), 8);
+  a->sink_slices = (int32_t)max64(1, min64((walk_sink + goal - 1) / goal, 256));
+  a->slices = (int32_t)max64(1, min64((walk + goal - 1) / goal, 256));
+  return 2 * (int64_t)a->B * a->H * a->stat_rows + 32 + dkv_parts(*a) * a->B * a->Hkv * (2 * kKeys * d);
 }
 
 hipError_t launch_window_backward(int dtype, int d, const WindowArgs& args, hipStream_t s) {
   WindowArgs a = args;
-  const BackwardPlan p = plan_backward(a, d);
-  a.ntiles = p.ntiles;
-  a.nktiles = p.nktiles;
-  a.stat_rows = p.stat_rows;
+  plan_backward(&a, d);
+  a.part = a.stats + 2 * (int64_t)a.B * a.H * a.stat_rows + 32;
   if (dtype == kBf16) return d == 128 ? launch<__bf16, 128>(a, s) : launch<__bf16, 64>(a, s);
   return d == 128 ? launch<_Float16, 128>(a, s) : launch<_Float16, 64>(a, s);
 }
