@@ -9,7 +9,12 @@
 // rows - touch every bank.
 #pragma once
 
+#include <type_traits>
+#include <utility>
+
 #include "ops_internal.h"
+
+#define BSA_INLINE __attribute__((always_inline))
 
 namespace bsa_ops {
 namespace {
@@ -66,6 +71,13 @@ template <int N>
 __device__ inline void wait_vm_lgkm() {
   static_assert(N >= 0 && N < 64, "vmcnt range");
   __builtin_amdgcn_s_waitcnt(0x0070 | (N & 15) | ((N >> 4) << 14));
+}
+
+// The same for vector memory alone.
+template <int N>
+__device__ inline void wait_vm() {
+  static_assert(N >= 0 && N < 64, "vmcnt range");
+  __builtin_amdgcn_s_waitcnt(0x0F70 | (N & 15) | ((N >> 4) << 14));
 }
 
 // Workgroup barrier without a memory fence: what the LDS loads wrote is complete
@@ -137,16 +149,21 @@ struct TileLoad {
       offs[j] = (uint32_t)r * stride + (((lane % R::kChunks) ^ R::swizzle(r & 15)) << 4);
     }
   }
-  // `rows` valid rows (may be 0 or less, or more than TR) from `base` on
-  __device__ void issue(const char* base, int rows, uint8_t* lds, int w) const {
+  // descriptor of `rows` valid rows (may be 0 or less, or more than TR) from `base` on
+  __device__ __amdgpu_buffer_rsrc_t rsrc(const char* base, int rows) const {
     const int n = rows < TR ? rows : TR;
     const uint32_t bytes = n > 0 ? (uint32_t)(n - 1) * stride + R::kBytes : 0;
-    const __amdgpu_buffer_rsrc_t rsrc = __builtin_amdgcn_make_buffer_rsrc(const_cast<char*>(base), 0, (int)bytes, 0x00020000);
+    return __builtin_amdgcn_make_buffer_rsrc(const_cast<char*>(base), 0, (int)bytes, 0x00020000);
+  }
+  __device__ void one(__amdgpu_buffer_rsrc_t r, int j, uint8_t* lds, int w) const {
+    __builtin_amdgcn_raw_ptr_buffer_load_lds(
+        r, (__attribute__((address_space(3))) void*)(lds + 1024 * (w + j * NW)), 16,
+        offs[j % kOffs] + (uint32_t)((j / kOffs) * kOffs * NW * R::kPerLoad) * stride, 0, 0, 0);
+  }
+  __device__ void issue(const char* base, int rows, uint8_t* lds, int w) const {
+    const __amdgpu_buffer_rsrc_t r = rsrc(base, rows);
 #pragma unroll
-    for (int j = 0; j < kLoads; ++j)
-      __builtin_amdgcn_raw_ptr_buffer_load_lds(
-          rsrc, (__attribute__((address_space(3))) void*)(lds + 1024 * (w + j * NW)), 16,
-          offs[j % kOffs] + (uint32_t)((j / kOffs) * kOffs * NW * R::kPerLoad) * stride, 0, 0, 0);
+    for (int j = 0; j < kLoads; ++j) one(r, j, lds, w);
   }
 };
 
@@ -162,6 +179,18 @@ struct Seq {
   __device__ int lo(const WindowArgs& a, int i) const { return max(i + off - a.left, 0); }
   __device__ int hi(const WindowArgs& a, int i) const { return min(i + off + a.right, kv_len - 1); }
 };
+
+// f(0), f(1), ... f(N - 1) with constant arguments, as long as f returns true.  A
+// large loop body under #pragma unroll may be unrolled in part only, and ring
+// slots that are not constants make the compiler wait for every load in flight.
+template <class F, int... I>
+__device__ BSA_INLINE inline bool each_slot(F&& f, std::integer_sequence<int, I...>) {
+  return (f(std::integral_constant<int, I>{}) && ...);
+}
+template <int N, class F>
+__device__ BSA_INLINE inline bool each_slot(F&& f) {
+  return each_slot(f, std::make_integer_sequence<int, N>{});
+}
 
 // Bits below x of a 32-bit word.
 __device__ inline uint32_t bits_below(int x) { return x <= 0 ? 0u : x >= 32 ? ~0u : (1u << x) - 1u; }

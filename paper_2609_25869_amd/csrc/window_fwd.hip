@@ -17,6 +17,62 @@ namespace bsa_ops {
 namespace {
 
 constexpr int kMaxSplit = 64;
+constexpr float kSlack = 8.f;
+
+// Inline asm must not read a matrix instruction's result too early: the compiler
+// keeps the required distance for its own instructions only.
+template <int N>
+__device__ inline void settle(f32x16 (&x)[N]) {
+  static_assert(N == 1 || N == 2, "score blocks of a tile");
+  if constexpr (N == 1) asm volatile("s_nop 15\n\ts_nop 7" : "+v"(x[0]));
+  else asm volatile("s_nop 15\n\ts_nop 7" : "+v"(x[0]), "+v"(x[1]));
+}
+
+// Maximum of three numbers; of NaN and a number, the number.
+__device__ inline float max3(float a, float b, float c) {
+  float r;
+  asm("v_max3_f32 %0, %1, %2, %3" : "=v"(r) : "v"(a), "v"(b), "v"(c));
+  return r;
+}
+
+// Ends a wave's work: O and LSE of its rows, or the state of its slice of the keys
+// for the join.
+template <typename T, int D>
+__device__ inline void store_rows(const WindowArgs& a, const f32x16* o, float m, float l, bool live, int b, int bh, int qi,
+                                  int qh, int row, int split, int lane) {
+  using R = Rows<D>;
+  const int hh = lane >> 5;
+  l += other_half(l, lane);
+  if (!live) return;
+  if (a.nsplit == 1) {
+    const float inv = l > 0.f ? 1.f / l : 0.f;
+    T* op = static_cast<T*>(a.o) + b * a.os.b + qh * a.os.h + qi * a.os.n;
+#pragma unroll
+    for (int d = 0; d < R::kBlocks; ++d) {
+#pragma unroll
+      for (int g = 0; g < 4; ++g) {
+        u32x2 v;
+        v[0] = pack2<T>(o[d][4 * g] * inv, o[d][4 * g + 1] * inv);
+        v[1] = pack2<T>(o[d][4 * g + 2] * inv, o[d][4 * g + 3] * inv);
+        *reinterpret_cast<u32x2*>(op + d * 32 + 8 * g + 4 * hh) = v;
+      }
+    }
+    if (a.lse && hh == 0) a.lse[((int64_t)b * a.H + qh) * a.Nq + qi] = l > 0.f ? (m + __log2f(l)) * kLn2 : kNegInf;
+  } else {
+    // state of the slice: [row][slice] of O, then of (m, l)
+    const int64_t rows = (int64_t)a.B * a.Hkv * a.Nq * a.group;
+    const int64_t at = ((int64_t)bh * a.Nq * a.group + row) * a.nsplit + split;
+    float* po = a.part + at * D;
+#pragma unroll
+    for (int d = 0; d < R::kBlocks; ++d) {
+#pragma unroll
+      for (int g = 0; g < 4; ++g)
+        *reinterpret_cast<f32x4*>(po + d * 32 + 8 * g + 4 * hh) =
+            f32x4{o[d][4 * g], o[d][4 * g + 1], o[d][4 * g + 2], o[d][4 * g + 3]};
+    }
+    if (hh == 0) *reinterpret_cast<f32x2*>(a.part + rows * a.nsplit * D + 2 * at) = f32x2{m, l};
+  }
+}
 
 template <typename T, int D, int NW>
 __global__ __launch_bounds__(64 * NW) void window_fwd_kernel(WindowArgs a) {
@@ -127,17 +183,25 @@ __global__ __launch_bounds__(64 * NW) void window_fwd_kernel(WindowArgs a) {
           for (int i = 0; i < 16; ++i) s[kb2][i] = (bits >> ((i >> 2) * 8 + (i & 3))) & 1u ? s[kb2][i] : kNegInf;
         }
       }
+      // The reference is raised only where the maximum passes it by more than 2^8:
+      // below that, sums in 32 bits and 16-bit probabilities hold them as well.
       float mx = kNegInf;
+      settle(s);
 #pragma unroll
       for (int kb2 = 0; kb2 < kNKB; ++kb2) {
 #pragma unroll
-        for (int i = 0; i < 16; ++i) mx = fmaxf(mx, s[kb2][i]);
+        for (int i = 0; i < 16; i += 2) mx = max3(mx, s[kb2][i], s[kb2][i + 1]);
       }
-      mx = fmaxf(mx, other_half(mx, lane)) * a.scale_log2;
-      const float m_new = fmaxf(m, mx);
-      const float ref = m_new == kNegInf ? 0.f : m_new;
-      const float alpha = fast_exp2(m - ref);
-      m = m_new;
+      mx = max3(mx, mx, other_half(mx, lane)) * a.scale_log2;
+      if (__ballot(mx > m + kSlack) != 0) {
+        const float m_new = mx > m + kSlack ? mx : m;  // (-inf + 8 is -inf: the first key counts)
+        const float alpha = m_new == m ? 1.f : fast_exp2(m - m_new);
+        m = m_new;
+        l *= alpha;
+#pragma unroll
+        for (int d = 0; d < R::kBlocks; ++d) o[d] *= alpha;
+      }
+      const float ref = m == kNegInf ? 0.f : m;
       u32x4 p[2 * kNKB];
       float sum = 0.f;
 #pragma unroll
@@ -150,9 +214,7 @@ __global__ __launch_bounds__(64 * NW) void window_fwd_kernel(WindowArgs a) {
           p[2 * kb2 + i / 8][(i % 8) / 2] = pack2<T>(p0, p1);
         }
       }
-      l = l * alpha + sum;
-#pragma unroll
-      for (int d = 0; d < R::kBlocks; ++d) o[d] *= alpha;
+      l += sum;
 #pragma unroll
       for (int c = 0; c < 2 * kNKB; ++c) {
 #pragma unroll
@@ -164,36 +226,287 @@ __global__ __launch_bounds__(64 * NW) void window_fwd_kernel(WindowArgs a) {
   }
   wait_vm_lgkm<0>();  // no load may still write LDS when the workgroup ends
 
-  l += other_half(l, lane);
-  if (!live) return;
-  if (a.nsplit == 1) {
-    const float inv = l > 0.f ? 1.f / l : 0.f;
-    T* op = static_cast<T*>(a.o) + b * a.os.b + qh * a.os.h + qi * a.os.n;
+  store_rows<T, D>(a, o, m, l, live, b, bh, qi, qh, row, split, lane);
+#endif
+}
+
+// x = keep ? x : -inf, in place (keep is per lane).  The tied operand pins the
+// result to its register: written plainly, the compiler copies the scores on the
+// common path, where nothing is masked.
+__device__ inline void mask_inplace(float& x, bool keep) {
+  const float ninf = kNegInf;
+  asm volatile("v_cndmask_b32_e64 %0, %1, %0, %2" : "+v"(x) : "v"(ninf), "s"(__ballot(keep)));
+}
+
+// The kernel for 128-row tiles of head dim 128: four waves of 32 rows, tiles of 64
+// keys, two workgroups per CU.  The vector unit has nearly as much to do as the
+// matrix unit (per score an fma, an exponential at a quarter of the rate, an add
+// and half a conversion: 26 of the 32 cycles of its share of the products), so the
+// two overlap within a wave: an iteration computes the scores of tile t + 1 and
+// O += P V of tile t - 1 while it forms the probabilities of tile t, one
+// exponential per matrix instruction.
+//
+// The reference that a row's probabilities are formed against is not moved tile by
+// tile: they are formed against the current one, and their sum is checked before
+// any product uses them.  Only where it passes 2^8 (or is NaN), or the row meets its
+// first key, the reference is raised to the row's maximum, O is rescaled and the
+// probabilities are formed again.  That and the masking of the next tile's scores
+// share one rare branch: with one for each, the state no longer fits the registers.
+//
+// Slot j of the ring holds K of a tile x = j (mod 2) and V of tile x - 2: iteration
+// t reads slot t + 1 (mod 2) and refills the other.
+//
+// 115200 queries, 24 heads, 14401 keys around each and 3600 sinks: 20.6 ms (1190
+// TFLOP/s of visible pairs; the same work without the overlap within a wave 23.2 ms;
+// eight waves and 256 rows 21.1; two groups of 32 rows per wave, which halve the LDS
+// reads but leave one wave per SIMD, 23.7; 32-key tiles 21.6).
+template <typename T, int D>
+__global__ __launch_bounds__(256) __attribute__((amdgpu_waves_per_eu(2, 2)))
+void window_fwd_piped_kernel(WindowArgs a) {
+#ifdef __HIP_DEVICE_COMPILE__
+  using E = Elem<T>;
+  using R = Rows<D>;
+  typedef typename E::x8 x8;
+  constexpr int NW = 4, TQ = 32 * NW, TK = 64, kStages = 2;
+  constexpr int kNKB = TK / 32, kTile = TK * R::kBytes;
+  using Load = TileLoad<D, TK, NW>;
+  constexpr int kLoads = Load::kLoads, kGroup = 2 * kLoads;
+  __shared__ __attribute__((aligned(1024))) uint8_t ring0[2 * kTile];
+  __shared__ __attribute__((aligned(1024))) uint8_t ring1[2 * kTile];
+  auto kslot = [&](int i) BSA_INLINE -> uint8_t* { return i == 0 ? ring0 : ring1; };
+  auto vslot = [&](int i) BSA_INLINE -> uint8_t* { return kslot(i) + kTile; };
+
+  const int64_t item = item_of_slot(blockIdx.x, (int64_t)a.ntiles * a.nsplit * a.B * a.Hkv);
+  const int split = (int)(item % a.nsplit);
+  const int64_t rest = item / a.nsplit;
+  const int tile = (int)(rest % a.ntiles), bh = (int)(rest / a.ntiles);
+  const int b = bh / a.Hkv, kvh = bh % a.Hkv;
+  const Seq sq(a, b);
+  const int nrows = sq.q_len * a.group, r0 = tile * TQ;
+  if (r0 >= nrows) return;
+  KeyTiles kt;
+  kt.init<TK>(a, sq, r0 / a.group, (min(r0 + TQ, nrows) - 1) / a.group);
+  const int t_begin = (int)((int64_t)kt.nt * split / a.nsplit), t_end = (int)((int64_t)kt.nt * (split + 1) / a.nsplit);
+
+  const int tid = threadIdx.x, lane = tid & 63;
+  const int w = __builtin_amdgcn_readfirstlane(tid >> 6);
+  const int n = lane & 31, hh = lane >> 5;
+  const int rw = r0 + 32 * w;  // the wave's first row
+  const int row = rw + n;
+  const bool live = row < nrows;
+  const int qi = live ? row / a.group : 0, qh = kvh * a.group + (live ? row % a.group : 0);
+  const int lo = sq.lo(a, qi), hi = live ? sq.hi(a, qi) : -1;
+  x8 qf[R::kSteps];
+  {
+    const T* qp = static_cast<const T*>(a.q) + b * a.qs.b + qh * a.qs.h + qi * a.qs.n;
 #pragma unroll
-    for (int d = 0; d < R::kBlocks; ++d) {
+    for (int c = 0; c < R::kSteps; ++c) qf[c] = *reinterpret_cast<const x8*>(qp + 16 * c + 8 * hh);
+  }
+  // tiles that need no mask for any row of the wave
+  const int wave_last = min(rw + 31, nrows - 1);
+  const int full_lo = wave_last >= rw ? sq.lo(a, wave_last / a.group) : kFar;
+  const int full_hi = wave_last >= rw ? sq.hi(a, rw / a.group) : -1;
+  auto all_seen = [&](int j0) BSA_INLINE -> bool {
+    return (j0 >= full_lo || j0 + TK <= a.sinks) && j0 + TK - 1 <= full_hi;
+  };
+
+  Load lk, lv;
+  lk.init(a.ks.n, w, lane);
+  lv.init(a.vs.n, w, lane);
+  const char* kb = reinterpret_cast<const char*>(static_cast<const T*>(a.k) + b * a.ks.b + kvh * a.ks.h);
+  const char* vb = reinterpret_cast<const char*>(static_cast<const T*>(a.v) + b * a.vs.b + kvh * a.vs.h);
+  // tiles past the last load no row
+  auto k_rsrc = [&](int t) BSA_INLINE {
+    const int j = kt.key<TK>(t);
+    return lk.rsrc(kb + (int64_t)j * a.ks.n * 2, t < t_end ? kt.limit(t) - j : 0);
+  };
+  auto v_rsrc = [&](int t) BSA_INLINE {
+    const int j = kt.key<TK>(t);
+    return lv.rsrc(vb + (int64_t)j * a.vs.n * 2, t < t_end ? kt.limit(t) - j : 0);
+  };
+
+  int koff[R::kSteps], voff[2][R::kBlocks];
 #pragma unroll
-      for (int g = 0; g < 4; ++g) {
-        u32x2 v;
-        v[0] = pack2<T>(o[d][4 * g] * inv, o[d][4 * g + 1] * inv);
-        v[1] = pack2<T>(o[d][4 * g + 2] * inv, o[d][4 * g + 3] * inv);
-        *reinterpret_cast<u32x2*>(op + d * 32 + 8 * g + 4 * hh) = v;
+  for (int c = 0; c < R::kSteps; ++c) koff[c] = R::row_read(lane, c);
+#pragma unroll
+  for (int r = 0; r < 2; ++r) {
+#pragma unroll
+    for (int d = 0; d < R::kBlocks; ++d) voff[r][d] = R::tr_read(lane, r, d);
+  }
+
+  f32x16 o[R::kBlocks];
+#pragma unroll
+  for (int d = 0; d < R::kBlocks; ++d) o[d] = f32x16{};
+  float m_run = kNegInf, l_run = 0.f;
+
+  // Operands of one iteration: units [0, kNA) are the scores of the next tile,
+  // [kNA, kNU) O += P V of the previous one.
+  constexpr int kNA = R::kSteps * kNKB, kNB = R::kBlocks * (TK / 16), kNU = kNA + kNB;
+  auto load_op = [&](int u, const uint8_t* ks, const uint8_t* vs) BSA_INLINE -> x8 {
+    if (u < kNA) return *reinterpret_cast<const x8*>(ks + (u % kNKB) * 32 * R::kBytes + koff[u / kNKB]);
+    const int j = u - kNA, c = j / R::kBlocks, d = j % R::kBlocks;
+    return read_tr_pair<T>(vs + c * 16 * R::kBytes + voff[0][d], vs + c * 16 * R::kBytes + voff[1][d]);
+  };
+  constexpr int kE = 16 * kNKB, kChunks = TK / 16;  // scores of a lane, chunks of 8 probabilities
+  constexpr int kDmaEvery = kNU / kGroup;
+  static_assert(kDmaEvery >= 1, "refill loads must fit the units");
+  constexpr int kAhead = 3;
+  auto a_end = [&](int u) BSA_INLINE -> int { return u < 0 ? 0 : u < kNU - 1 ? (u + 1) * kE / (kNU - 1) : kE; };
+  constexpr float kSumMax = 256.f;
+  const float c_log2 = a.scale_log2;
+
+  auto apply_mask = [&](f32x16* s, int j0) BSA_INLINE {
+#pragma unroll
+    for (int kb2 = 0; kb2 < kNKB; ++kb2) {
+      const uint32_t mine = visible_bits(j0 + 32 * kb2, lo, hi, a.sinks) >> (4 * hh);
+#pragma unroll
+      for (int i = 0; i < 16; ++i) {
+        float x = s[kb2][i];
+        mask_inplace(x, (mine >> ((i >> 2) * 8 + (i & 3))) & 1u);
+        s[kb2][i] = x;
       }
     }
-    if (a.lse && hh == 0) a.lse[((int64_t)b * a.H + qh) * a.Nq + qi] = l > 0.f ? (m + __log2f(l)) * kLn2 : kNegInf;
-  } else {
-    // state of the slice: [row][slice] of O, then of (m, l)
-    const int64_t rows = (int64_t)a.B * a.Hkv * a.Nq * a.group;
-    const int64_t at = ((int64_t)bh * a.Nq * a.group + row) * a.nsplit + split;
-    float* po = a.part + at * D;
+  };
+  auto exponent = [&](float sv, float nm) BSA_INLINE { return fast_exp2(__builtin_fmaf(sv, c_log2, nm)); };
+
+  // Scores of tile t + 1 into s_nxt, O += P V of tile t - 1, the probabilities of
+  // tile t (scores s_cur) into pw_cur; returns the lane's sum of them.
+  auto iteration = [&](const f32x16* s_cur, f32x16* s_nxt, const uint8_t* ks_next, const uint8_t* vs_prev, u32x4* pw_cur,
+                       const u32x4* pw_prev, int t, uint8_t* k_refill, uint8_t* v_refill) BSA_INLINE -> float {
+    const float nm = m_run == kNegInf ? 0.f : -m_run;
+    const __amdgpu_buffer_rsrc_t kr = k_rsrc(t + kStages), vr = v_rsrc(t + kStages - 2);
+    float ls[2] = {0.f, 0.f};
+    float pf[kE];
+    auto stage_a = [&](int e) BSA_INLINE { pf[e] = exponent(s_cur[e / 16][e % 16], nm); };
+    auto stage_b = [&](int pr) BSA_INLINE {
+      const int e0 = 2 * pr;
+      uint32_t pair = pack2<T>(pf[e0], pf[e0 + 1]);
+      float& acc = ls[pr & 1];
+      acc += pf[e0] + pf[e0 + 1];
+      // keep both here: otherwise they are sunk past the check of the sum, and every
+      // probability is held in 32 bits until then
+      asm volatile("" : "+v"(acc), "+v"(pair));
+      pw_cur[e0 / 8][(e0 % 8) / 2] = pair;
+    };
+    x8 op[kAhead + 1];
 #pragma unroll
-    for (int d = 0; d < R::kBlocks; ++d) {
+    for (int u = 0; u < kAhead; ++u) op[u] = load_op(u, ks_next, vs_prev);
 #pragma unroll
-      for (int g = 0; g < 4; ++g)
-        *reinterpret_cast<f32x4*>(po + d * 32 + 8 * g + 4 * hh) =
-            f32x4{o[d][4 * g], o[d][4 * g + 1], o[d][4 * g + 2], o[d][4 * g + 3]};
+    for (int u = 0; u < kNU; ++u) {
+      if (u + kAhead < kNU) op[(u + kAhead) % (kAhead + 1)] = load_op(u + kAhead, ks_next, vs_prev);
+      if (u % kDmaEvery == 0 && u / kDmaEvery < kGroup) {
+        const int i = u / kDmaEvery;
+        if (i < kLoads) lk.one(kr, i, k_refill, w);
+        else lv.one(vr, i - kLoads, v_refill, w);
+      }
+      if (u < kNA) {
+        f32x16& acc = s_nxt[u % kNKB];
+        acc = E::mfma(op[u % (kAhead + 1)], qf[u / kNKB], u < kNKB ? f32x16{} : acc);
+      } else {
+        const int j = u - kNA, d = j % R::kBlocks;
+        o[d] = E::mfma(op[u % (kAhead + 1)], __builtin_bit_cast(x8, pw_prev[j / R::kBlocks]), o[d]);
+      }
+      // a pair is packed one step after its exponentials, so nothing waits for one
+#pragma unroll
+      for (int pr = a_end(u - 2) / 2; pr < a_end(u - 1) / 2; ++pr) stage_b(pr);
+#pragma unroll
+      for (int e = a_end(u - 1); e < a_end(u); ++e) stage_a(e);
+      __builtin_amdgcn_sched_barrier(0);
     }
-    if (hh == 0) *reinterpret_cast<f32x2*>(a.part + rows * a.nsplit * D + 2 * at) = f32x2{m, l};
+#pragma unroll
+    for (int pr = a_end(kNU - 2) / 2; pr < kE / 2; ++pr) stage_b(pr);
+    return ls[0] + ls[1];
+  };
+
+  // For the flagged rows: raise the reference to the maximum so far, rescale O and
+  // l, and form the tile's probabilities again.  Other rows keep theirs to the bit.
+  auto raise_reference = [&](const f32x16* s_cur, u32x4* pw_cur, bool mine, float sum_old) BSA_INLINE -> float {
+    float mx = kNegInf;
+#pragma unroll
+    for (int kb2 = 0; kb2 < kNKB; ++kb2) {
+#pragma unroll
+      for (int i = 0; i < 16; i += 2) mx = max3(mx, s_cur[kb2][i], s_cur[kb2][i + 1]);
+    }
+    mx = max3(mx, mx, other_half(mx, lane)) * c_log2;
+    const float m_new = mine ? max3(m_run, m_run, mx) : m_run;
+    const float alpha = m_new == m_run ? 1.f : fast_exp2(m_run - m_new);
+    m_run = m_new;
+    l_run *= alpha;
+#pragma unroll
+    for (int d = 0; d < R::kBlocks; ++d) o[d] *= alpha;
+    const float nm = m_new == kNegInf ? 0.f : -m_new;
+    float ls[2] = {0.f, 0.f};
+#pragma unroll
+    for (int pr = 0; pr < kE / 2; ++pr) {
+      const int e0 = 2 * pr;
+      const float p0 = exponent(s_cur[e0 / 16][e0 % 16], nm), p1 = exponent(s_cur[e0 / 16][e0 % 16 + 1], nm);
+      pw_cur[e0 / 8][(e0 % 8) / 2] = pack2<T>(p0, p1);
+      ls[pr & 1] += p0 + p1;
+    }
+    return mine ? ls[0] + ls[1] : sum_old;
+  };
+
+  f32x16 sA[kNKB], sB[kNKB];
+  u32x4 pwA[kChunks], pwB[kChunks];
+#pragma unroll
+  for (int c = 0; c < kChunks; ++c) pwB[c] = u32x4{};  // P of the tile before the first
+  if (t_begin < t_end) {
+    // slot 0 <- K of the first tile; slot 1 <- K of the next one, and the first V, which
+    // the zeros of pwB multiply
+    lk.issue(kb + (int64_t)kt.key<TK>(t_begin) * a.ks.n * 2, kt.limit(t_begin) - kt.key<TK>(t_begin), kslot(0), w);
+    const __amdgpu_buffer_rsrc_t kr = k_rsrc(t_begin + 1), vr = v_rsrc(t_begin);
+#pragma unroll
+    for (int j = 0; j < kLoads; ++j) lk.one(kr, j, kslot(1), w);
+#pragma unroll
+    for (int j = 0; j < kLoads; ++j) lv.one(vr, j, vslot(1), w);
+    wait_vm_lgkm<kGroup>();
+    block_sync();
+#pragma unroll
+    for (int u = 0; u < kNA; ++u) {
+      f32x16& acc = sA[u % kNKB];
+      acc = E::mfma(load_op(u, kslot(0), nullptr), qf[u / kNKB], u < kNKB ? f32x16{} : acc);
+    }
+    settle(sA);
+    apply_mask(sA, kt.key<TK>(t_begin));
+    wait_vm_lgkm<0>();
+    block_sync();  // every wave has read slot 0 before it is refilled
   }
+  for (int t0 = t_begin; t0 < t_end; t0 += kStages) {
+    each_slot<kStages>([&](auto slot) BSA_INLINE -> bool {
+      constexpr int u = decltype(slot)::value;
+      const int t = t0 + u;
+      if (t >= t_end) return false;
+      f32x16* s_cur = u == 0 ? sA : sB;
+      f32x16* s_nxt = u == 0 ? sB : sA;
+      u32x4* pw_cur = u == 0 ? pwA : pwB;
+      float sum = iteration(s_cur, s_nxt, kslot(1 - u), vslot(1 - u), pw_cur, u == 0 ? pwB : pwA, t, kslot(u), vslot(u));
+      // (the sum is >= 0 or NaN, which as an integer is above every number)
+      const int j0 = kt.key<TK>(t), j1 = kt.key<TK>(t + 1);
+      const bool raise = __float_as_uint(sum) > __float_as_uint(kSumMax) ||
+                         (m_run == kNegInf && j0 <= hi && (j0 + TK > lo || j0 < a.sinks));
+      if (__builtin_expect(__ballot(raise) != 0 || !all_seen(j1), 0)) {
+        // both halves of a row take the same decision
+        const float mine = raise ? 1.f : 0.f;
+        sum = raise_reference(s_cur, pw_cur, mine + other_half(mine, lane) > 0.f, sum);
+        apply_mask(s_nxt, j1);
+      }
+      l_run += sum;
+      wait_vm_lgkm<0>();
+      block_sync();
+      return true;
+    });
+  }
+  if (t_begin < t_end) {
+    // O += P V of the last tile
+    const bool even = (t_end - 1 - t_begin) % 2 == 0;
+    const u32x4* pw_last = even ? pwA : pwB;
+    const uint8_t* vs = even ? vslot(0) : vslot(1);
+#pragma unroll
+    for (int j = 0; j < kNB; ++j)
+      o[j % R::kBlocks] = E::mfma(load_op(kNA + j, nullptr, vs), __builtin_bit_cast(x8, pw_last[j / R::kBlocks]), o[j % R::kBlocks]);
+  }
+  wait_vm_lgkm<0>();  // no load may still write LDS when the workgroup ends
+  store_rows<T, D>(a, o, m_run, l_run, live, b, bh, qi, qh, row, split, lane);
 #endif
 }
 
@@ -256,6 +569,8 @@ hipError_t launch(const WindowArgs& a, const ForwardPlan& p, hipStream_t s) {
   if (n > 0x7fffffff) return hipErrorInvalidValue;
   if (p.tile_rows == 32)
     hipLaunchKernelGGL((window_fwd_kernel<T, D, 1>), dim3((unsigned)n), dim3(64), 0, s, a);
+  else if constexpr (D == 128)
+    hipLaunchKernelGGL((window_fwd_piped_kernel<T, D>), dim3((unsigned)n), dim3(256), 0, s, a);
   else
     hipLaunchKernelGGL((window_fwd_kernel<T, D, 4>), dim3((unsigned)n), dim3(256), 0, s, a);
   hipError_t e = hipGetLastError();

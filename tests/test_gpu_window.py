@@ -46,6 +46,12 @@ CASES = {
     "ragged_f": (3, 5, 1, 150, 150, 64, 33, 0, 1, [150, 149, 2], [150, 149, 2]),
     "group_7": (1, 7, 1, 65, 65, 64, 31, 0, 0, None, None),
     "group_16": (1, 16, 1, 40, 140, 128, 70, 3, 6, None, None),
+    # enough rows for the kernel of 256-row tiles
+    "many_rows": (4, 64, 64, 300, 300, 128, 90, 0, 5, None, None),
+    "many_rows_shared": (8, 64, 32, 170, 210, 64, 45, 20, 33, [170, 1, 0, 99, 170, 30, 128, 129],
+                         [210, 1, 50, 60, 210, 200, 128, 170]),
+    "many_rows_group_16": (16, 256, 16, 30, 130, 128, 64, 0, 1, None, None),
+    "many_rows_all_keys": (2, 128, 128, 257, 257, 64, -1, 0, 0, None, None),
     "no_keys": (2, 2, 1, 5, 0, 64, 4, 0, 1, None, None),
     "no_queries": (1, 2, 1, 0, 20, 64, 4, 0, 1, None, None),
     "lengths_out_of_range": (3, 2, 1, 20, 30, 64, 6, 0, 1, [25, -3, 20], [99, 30, -1]),
