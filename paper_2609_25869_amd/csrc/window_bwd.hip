@@ -93,14 +93,9 @@ __global__ __launch_bounds__(64 * kWaves) void window_dq_kernel(WindowArgs a) {
     lk.issue(kb + (int64_t)j * a.ks.n * 2, rows, s, w);
     lv.issue(vb + (int64_t)j * a.vs.n * 2, rows, s + kTile, w);
   };
-  int roff[R::kSteps], toff[2][R::kBlocks];
-#pragma unroll
-  for (int c = 0; c < R::kSteps; ++c) roff[c] = R::row_read(lane, c);
-#pragma unroll
-  for (int r = 0; r < 2; ++r) {
-#pragma unroll
-    for (int d = 0; d < R::kBlocks; ++d) toff[r][d] = R::tr_read(lane, r, d);
-  }
+  // (chunk c of a row, and column block d, differ from the first by bits that the
+  // swizzle only flips)
+  const int roff = R::row_read(lane, 0), toff0 = R::tr_read(lane, 0, 0), toff1 = R::tr_read(lane, 1, 0);
   f32x16 acc[R::kBlocks];
 #pragma unroll
   for (int d = 0; d < R::kBlocks; ++d) acc[d] = f32x16{};
@@ -112,31 +107,33 @@ __global__ __launch_bounds__(64 * kWaves) void window_dq_kernel(WindowArgs a) {
 #pragma unroll
     for (int s = 0; s < kStages - 1; ++s) issue(s, slot(s));
   }
-  for (int t0 = 0; t0 < kt.nt; t0 += kStages) {
+  for (int tb = 0; tb < kt.nt; tb += kStages) {
 #pragma unroll
     for (int u = 0; u < kStages; ++u) {
-      const int t = t0 + u;
+      const int t = tb + u;
       if (t >= kt.nt) break;
       wait_vm_lgkm<(kStages - 2) * kGroup>();
       block_sync();
       issue(t + kStages - 1, slot((u + kStages - 1) % kStages));
       const uint8_t* ks = slot(u);
       const uint8_t* vs = ks + kTile;
+      int ro = roff, t0 = toff0, t1 = toff1;
+      asm volatile("" : "+v"(ro), "+v"(t0), "+v"(t1));  // formed again per tile: sixteen addresses would not fit
       const int j0 = kt.key<TK>(t);
       f32x16 s = {}, dp = {};
 #pragma unroll
       for (int c = 0; c < R::kSteps; ++c) {
-        s = E::mfma(*reinterpret_cast<const x8*>(ks + roff[c]), qf[c], s);
-        dp = E::mfma(*reinterpret_cast<const x8*>(vs + roff[c]), df[c], dp);
+        s = E::mfma(*reinterpret_cast<const x8*>(ks + (ro ^ (c << 5))), qf[c], s);
+        dp = E::mfma(*reinterpret_cast<const x8*>(vs + (ro ^ (c << 5))), df[c], dp);
       }
       float ds[16];
 #pragma unroll
       for (int i = 0; i < 16; ++i) ds[i] = fast_exp2(__builtin_fmaf(s[i], a.scale_log2, -lse)) * (dp[i] - delta);
       const bool full = (j0 >= full_lo || j0 + TK <= a.sinks) && j0 + TK - 1 <= full_hi;
-      if (!full) {
+      if (__builtin_expect(!full, 0)) {
         const uint32_t bits = visible_bits(j0, lo, hi, a.sinks) >> (4 * hh);
 #pragma unroll
-        for (int i = 0; i < 16; ++i) ds[i] = (bits >> ((i >> 2) * 8 + (i & 3))) & 1u ? ds[i] : 0.f;
+        for (int i = 0; i < 16; ++i) zero_unless(ds[i], (bits >> ((i >> 2) * 8 + (i & 3))) & 1u);
       }
       u32x4 p[2];
 #pragma unroll
@@ -145,7 +142,7 @@ __global__ __launch_bounds__(64 * kWaves) void window_dq_kernel(WindowArgs a) {
       for (int c = 0; c < 2; ++c) {
 #pragma unroll
         for (int d = 0; d < R::kBlocks; ++d)
-          acc[d] = E::mfma(read_tr_pair<T>(ks + c * 16 * R::kBytes + toff[0][d], ks + c * 16 * R::kBytes + toff[1][d]),
+          acc[d] = E::mfma(read_tr_pair<T>(ks + c * 16 * R::kBytes + (t0 ^ (d << 6)), ks + c * 16 * R::kBytes + (t1 ^ (d << 6))),
                            __builtin_bit_cast(x8, p[c]), acc[d]);
       }
     }
@@ -180,7 +177,7 @@ struct Seen {
 };
 
 template <typename T, int D>
-__global__ __launch_bounds__(64 * kWaves) void window_dkv_kernel(WindowArgs a) {
+__global__ __launch_bounds__(64 * kWaves) __attribute__((amdgpu_waves_per_eu(2, 2))) void window_dkv_kernel(WindowArgs a) {
 #ifdef __HIP_DEVICE_COMPILE__
   using E = Elem<T>;
   using R = Rows<D>;
@@ -217,14 +214,10 @@ __global__ __launch_bounds__(64 * kWaves) void window_dkv_kernel(WindowArgs a) {
 
   const int tid = threadIdx.x, lane = tid & 63;
   const int w = __builtin_amdgcn_readfirstlane(tid >> 6);
-  const int n = lane & 31, hh = lane >> 5;
-  const int key = k0 + 32 * w + n;
-  const bool live = key < sq.kv_len;
-  const int first = seen.first(key), last = seen.last(key);
 
   x8 kf[R::kSteps], vf[R::kSteps];
   {
-    const int at = live ? key : k0;
+    const int own = k0 + 32 * w + (lane & 31), at = own < sq.kv_len ? own : k0, hh = lane >> 5;
     const T* kp = static_cast<const T*>(a.k) + b * a.ks.b + kvh * a.ks.h + at * a.ks.n;
     const T* vp = static_cast<const T*>(a.v) + b * a.vs.b + kvh * a.vs.h + at * a.vs.n;
 #pragma unroll
@@ -240,13 +233,14 @@ __global__ __launch_bounds__(64 * kWaves) void window_dkv_kernel(WindowArgs a) {
   // the row tile that is loaded next, and the one that is worked on
   int g_in = per_head ? (int)(t_begin / per_head) : 0, i_in = i_lo + (per_head ? (int)(t_begin % per_head) : 0) * TR;
   int i_now = i_in;
-  const uint32_t stat_off = (uint32_t)(n * 4) + (hh ? (uint32_t)(a.stat_rows * 4) : 0u);
   auto issue = [&](uint8_t* s) {
     const bool any = g_in < a.group;
     const int qh = kvh * a.group + (any ? g_in : 0), rows = any ? i_hi + 1 - i_in : 0;
     lq.issue(reinterpret_cast<const char*>(static_cast<const T*>(a.q) + b * a.qs.b + qh * a.qs.h + i_in * a.qs.n), rows, s, w);
     ld.issue(reinterpret_cast<const char*>(static_cast<const T*>(a.dout) + b * a.dos.b + qh * a.dos.h + i_in * a.dos.n), rows,
              s + kTile, w);
+    const int l = lane_now();
+    const uint32_t stat_off = (uint32_t)(l & 31) * 4 + (l >> 5) * (uint32_t)(a.stat_rows * 4);
     const float* st = a.stats + ((int64_t)b * a.H + qh) * 2 * a.stat_rows + i_in;
     const __amdgpu_buffer_rsrc_t rsrc = __builtin_amdgcn_make_buffer_rsrc(
         const_cast<float*>(st), 0, any ? (int)((a.stat_rows + TR) * 4) : 0, 0x00020000);
@@ -259,14 +253,9 @@ __global__ __launch_bounds__(64 * kWaves) void window_dkv_kernel(WindowArgs a) {
     }
   };
 
-  int roff[R::kSteps], toff[2][R::kBlocks];
-#pragma unroll
-  for (int c = 0; c < R::kSteps; ++c) roff[c] = R::row_read(lane, c);
-#pragma unroll
-  for (int r = 0; r < 2; ++r) {
-#pragma unroll
-    for (int d = 0; d < R::kBlocks; ++d) toff[r][d] = R::tr_read(lane, r, d);
-  }
+  // (chunk c of a row, and column block d, differ from the first by bits that the
+  // swizzle only flips)
+  const int roff = R::row_read(lane, 0), toff0 = R::tr_read(lane, 0, 0), toff1 = R::tr_read(lane, 1, 0);
   f32x16 dk[R::kBlocks], dv[R::kBlocks];
 #pragma unroll
   for (int d = 0; d < R::kBlocks; ++d) {
@@ -282,54 +271,61 @@ __global__ __launch_bounds__(64 * kWaves) void window_dkv_kernel(WindowArgs a) {
 #pragma unroll
     for (int s = 0; s < kStages - 1; ++s) issue(slot(s));
   }
-  for (int t0 = 0; t0 < nt; t0 += kStages) {
+  for (int tb = 0; tb < nt; tb += kStages) {
 #pragma unroll
     for (int u = 0; u < kStages; ++u) {
-      const int t = t0 + u;
+      const int t = tb + u;
       if (t >= nt) break;
       wait_vm_lgkm<(kStages - 2) * kGroup>();
       block_sync();
       issue(slot((u + kStages - 1) % kStages));
       const uint8_t* qs = slot(u);
       const uint8_t* gs = qs + kTile;
-      const uint8_t* st = qs + 2 * kTile + w * kStat + 16 * hh;
+      int ro = roff, t0 = toff0, t1 = toff1;
+      asm volatile("" : "+v"(ro), "+v"(t0), "+v"(t1));  // formed again per tile: sixteen addresses would not fit
+      const uint8_t* st = qs + 2 * kTile + w * kStat + 16 * (lane_now() >> 5);
       f32x16 s = {}, dp = {};
 #pragma unroll
       for (int c = 0; c < R::kSteps; ++c) {
-        s = E::mfma(*reinterpret_cast<const x8*>(qs + roff[c]), kf[c], s);
-        dp = E::mfma(*reinterpret_cast<const x8*>(gs + roff[c]), vf[c], dp);
+        s = E::mfma(*reinterpret_cast<const x8*>(qs + (ro ^ (c << 5))), kf[c], s);
+        dp = E::mfma(*reinterpret_cast<const x8*>(gs + (ro ^ (c << 5))), vf[c], dp);
       }
       const bool full = i_now >= full_lo && i_now + TR - 1 <= full_hi;
-      uint32_t bits = ~0u;
-      if (!full) bits = (bits_below(last - i_now + 1) & ~bits_below(first - i_now)) >> (4 * hh);
-      u32x4 p[2], q[2];
+      float pv[16], ds[16];
 #pragma unroll
       for (int r4 = 0; r4 < 4; ++r4) {
         const f32x4 lse = *reinterpret_cast<const f32x4*>(st + 32 * r4);
         const f32x4 delta = *reinterpret_cast<const f32x4*>(st + 128 + 32 * r4);
-        float pv[4], dsv[4];
 #pragma unroll
         for (int e = 0; e < 4; ++e) {
           const int i = 4 * r4 + e;
-          pv[e] = fast_exp2(__builtin_fmaf(s[i], a.scale_log2, -lse[e]));
-          dsv[e] = pv[e] * (dp[i] - delta[e]);
-          if (!full) {
-            const bool see = (bits >> (8 * r4 + e)) & 1u;
-            pv[e] = see ? pv[e] : 0.f;
-            dsv[e] = see ? dsv[e] : 0.f;
-          }
+          pv[i] = fast_exp2(__builtin_fmaf(s[i], a.scale_log2, -lse[e]));
+          ds[i] = pv[i] * (dp[i] - delta[e]);
         }
+        __builtin_amdgcn_sched_barrier(0);
+      }
+      if (__builtin_expect(!full, 0)) {
+        const int l = lane_now(), key = kw + (l & 31);
+        const uint32_t bits =
+            (bits_below(seen.last(key) - i_now + 1) & ~bits_below(seen.first(key) - i_now)) >> (4 * (l >> 5));
 #pragma unroll
-        for (int e = 0; e < 4; e += 2) {
-          p[r4 / 2][(4 * (r4 % 2) + e) / 2] = pack2<T>(pv[e], pv[e + 1]);
-          q[r4 / 2][(4 * (r4 % 2) + e) / 2] = pack2<T>(dsv[e], dsv[e + 1]);
+        for (int i = 0; i < 16; ++i) {
+          const bool see = (bits >> (8 * (i >> 2) + (i & 3))) & 1u;
+          zero_unless(pv[i], see);
+          zero_unless(ds[i], see);
         }
+      }
+      u32x4 p[2], q[2];
+#pragma unroll
+      for (int i = 0; i < 16; i += 2) {
+        p[i / 8][(i % 8) / 2] = pack2<T>(pv[i], pv[i + 1]);
+        q[i / 8][(i % 8) / 2] = pack2<T>(ds[i], ds[i + 1]);
       }
 #pragma unroll
       for (int c = 0; c < 2; ++c) {
 #pragma unroll
         for (int d = 0; d < R::kBlocks; ++d) {
-          const int o0 = c * 16 * R::kBytes + toff[0][d], o1 = c * 16 * R::kBytes + toff[1][d];
+          const int o0 = c * 16 * R::kBytes + (t0 ^ (d << 6)), o1 = c * 16 * R::kBytes + (t1 ^ (d << 6));
           dv[d] = E::mfma(read_tr_pair<T>(gs + o0, gs + o1), __builtin_bit_cast(x8, p[c]), dv[d]);
           dk[d] = E::mfma(read_tr_pair<T>(qs + o0, qs + o1), __builtin_bit_cast(x8, q[c]), dk[d]);
         }
@@ -339,7 +335,8 @@ __global__ __launch_bounds__(64 * kWaves) void window_dkv_kernel(WindowArgs a) {
     }
   }
   wait_vm_lgkm<0>();
-  if (!live) return;
+  const int end_lane = lane_now(), key = kw + (end_lane & 31), hh = end_lane >> 5;
+  if (key >= sq.kv_len) return;
   if (nslice > 1) {
     // [slice][dK, dV][key][column]
     const int64_t first_part = sink || a.sink_slices == 1 ? 0 : (int64_t)a.nsink * a.sink_slices;

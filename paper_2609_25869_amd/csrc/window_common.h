@@ -226,6 +226,21 @@ struct KeyTiles {
   __device__ int limit(int t) const { return t < ns ? sink_end : end; }
 };
 
+// The lane index, formed again where it is used: rare paths and the ends of kernels
+// then keep no register for it through the loop.
+__device__ inline int lane_now() {
+  int l = __builtin_amdgcn_mbcnt_hi(~0u, __builtin_amdgcn_mbcnt_lo(~0u, 0u));
+  asm volatile("" : "+v"(l));
+  return l;
+}
+
+// x = keep ? x : 0 in place (keep is per lane), in a branch that is rarely taken: the
+// tied operand pins the result to its register, and the compiler cannot turn the
+// branch into selections that run every time.
+__device__ inline void zero_unless(float& x, bool keep) {
+  asm volatile("v_cndmask_b32_e64 %0, 0, %0, %1" : "+v"(x) : "s"(__ballot(keep)));
+}
+
 // Dispatch order: the eight XCDs take consecutive workgroups in turn, so slot s
 // runs work item (s % 8) * ceil(n / 8) + s / 8, which gives every XCD a
 // contiguous share of the items, in order: neighbouring row tiles of a head
