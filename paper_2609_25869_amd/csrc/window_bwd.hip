@@ -33,15 +33,13 @@ __global__ __launch_bounds__(64 * kWaves) void window_dq_kernel(WindowArgs a) {
   using E = Elem<T>;
   using R = Rows<D>;
   typedef typename E::x8 x8;
-  constexpr int TK = 32, TQ = 32 * kWaves, kStages = 4;
+  constexpr int TK = 64, TQ = 32 * kWaves, kStages = 2;
   constexpr int kTile = TK * R::kBytes;
   using Load = TileLoad<D, TK, kWaves>;
   constexpr int kGroup = 2 * Load::kLoads;
   __shared__ __attribute__((aligned(1024))) uint8_t ring0[2 * kTile];
   __shared__ __attribute__((aligned(1024))) uint8_t ring1[2 * kTile];
-  __shared__ __attribute__((aligned(1024))) uint8_t ring2[2 * kTile];
-  __shared__ __attribute__((aligned(1024))) uint8_t ring3[2 * kTile];
-  auto slot = [&](int i) -> uint8_t* { return i == 0 ? ring0 : i == 1 ? ring1 : i == 2 ? ring2 : ring3; };
+  auto slot = [&](int i) -> uint8_t* { return i == 0 ? ring0 : ring1; };
 
   const int64_t item = item_of_slot(blockIdx.x, (int64_t)a.ntiles * a.B * a.Hkv);
   const int tile = (int)(item % a.ntiles), bh = (int)(item / a.ntiles);
@@ -88,7 +86,7 @@ __global__ __launch_bounds__(64 * kWaves) void window_dq_kernel(WindowArgs a) {
   lv.init(a.vs.n, w, lane);
   const char* kb = reinterpret_cast<const char*>(static_cast<const T*>(a.k) + b * a.ks.b + kvh * a.ks.h);
   const char* vb = reinterpret_cast<const char*>(static_cast<const T*>(a.v) + b * a.vs.b + kvh * a.vs.h);
-  auto issue = [&](int t, uint8_t* s) {
+  auto issue = [&](int t, uint8_t* s) BSA_INLINE {
     const int j = kt.key<TK>(t), rows = t < kt.nt ? kt.limit(t) - j : 0;
     lk.issue(kb + (int64_t)j * a.ks.n * 2, rows, s, w);
     lv.issue(vb + (int64_t)j * a.vs.n * 2, rows, s + kTile, w);
@@ -108,18 +106,19 @@ __global__ __launch_bounds__(64 * kWaves) void window_dq_kernel(WindowArgs a) {
     for (int s = 0; s < kStages - 1; ++s) issue(s, slot(s));
   }
   for (int tb = 0; tb < kt.nt; tb += kStages) {
-#pragma unroll
-    for (int u = 0; u < kStages; ++u) {
+    each_slot<kStages>([&](auto at) BSA_INLINE -> bool {
+      constexpr int u = decltype(at)::value;
       const int t = tb + u;
-      if (t >= kt.nt) break;
+      if (t >= kt.nt) return false;
       wait_vm_lgkm<(kStages - 2) * kGroup>();
       block_sync();
       issue(t + kStages - 1, slot((u + kStages - 1) % kStages));
-      const uint8_t* ks = slot(u);
+      auto half = [&](auto blk) BSA_INLINE {
+      const uint8_t* ks = slot(u) + decltype(blk)::value * 32 * R::kBytes;
       const uint8_t* vs = ks + kTile;
       int ro = roff, t0 = toff0, t1 = toff1;
       asm volatile("" : "+v"(ro), "+v"(t0), "+v"(t1));  // formed again per tile: sixteen addresses would not fit
-      const int j0 = kt.key<TK>(t);
+      const int j0 = kt.key<TK>(t) + decltype(blk)::value * 32;
       f32x16 s = {}, dp = {};
 #pragma unroll
       for (int c = 0; c < R::kSteps; ++c) {
@@ -129,9 +128,10 @@ __global__ __launch_bounds__(64 * kWaves) void window_dq_kernel(WindowArgs a) {
       float ds[16];
 #pragma unroll
       for (int i = 0; i < 16; ++i) ds[i] = fast_exp2(__builtin_fmaf(s[i], a.scale_log2, -lse)) * (dp[i] - delta);
-      const bool full = (j0 >= full_lo || j0 + TK <= a.sinks) && j0 + TK - 1 <= full_hi;
+      const int last = kt.limit(t) - 1;
+      const bool full = (j0 >= full_lo || j0 + 32 <= a.sinks) && j0 + 31 <= min(full_hi, last);
       if (__builtin_expect(!full, 0)) {
-        const uint32_t bits = visible_bits(j0, lo, hi, a.sinks) >> (4 * hh);
+        const uint32_t bits = visible_bits(j0, lo, min(hi, last), a.sinks) >> (4 * hh);
 #pragma unroll
         for (int i = 0; i < 16; ++i) zero_unless(ds[i], (bits >> ((i >> 2) * 8 + (i & 3))) & 1u);
       }
@@ -145,7 +145,11 @@ __global__ __launch_bounds__(64 * kWaves) void window_dq_kernel(WindowArgs a) {
           acc[d] = E::mfma(read_tr_pair<T>(ks + c * 16 * R::kBytes + (t0 ^ (d << 6)), ks + c * 16 * R::kBytes + (t1 ^ (d << 6))),
                            __builtin_bit_cast(x8, p[c]), acc[d]);
       }
-    }
+      };
+      half(std::integral_constant<int, 0>{});
+      half(std::integral_constant<int, 1>{});
+      return true;
+    });
   }
   wait_vm_lgkm<0>();
   if (!live) return;
@@ -182,16 +186,14 @@ __global__ __launch_bounds__(64 * kWaves) __attribute__((amdgpu_waves_per_eu(2, 
   using E = Elem<T>;
   using R = Rows<D>;
   typedef typename E::x8 x8;
-  constexpr int TR = 32, TKEY = 32 * kWaves, kStages = 4;
-  constexpr int kTile = TR * R::kBytes, kStat = 256;
+  constexpr int TR = 64, TKEY = 32 * kWaves, kStages = 2;
+  constexpr int kTile = TR * R::kBytes, kStat = 512;
   using Load = TileLoad<D, TR, kWaves>;
-  constexpr int kGroup = 2 * Load::kLoads + 1;
+  constexpr int kGroup = 2 * Load::kLoads + 2;
   constexpr int kSlot = 2 * kTile + kWaves * kStat;  // Q, dO, and LSE and D of the rows, a copy per wave
   __shared__ __attribute__((aligned(1024))) uint8_t ring0[kSlot];
   __shared__ __attribute__((aligned(1024))) uint8_t ring1[kSlot];
-  __shared__ __attribute__((aligned(1024))) uint8_t ring2[kSlot];
-  __shared__ __attribute__((aligned(1024))) uint8_t ring3[kSlot];
-  auto slot = [&](int i) -> uint8_t* { return i == 0 ? ring0 : i == 1 ? ring1 : i == 2 ? ring2 : ring3; };
+  auto slot = [&](int i) -> uint8_t* { return i == 0 ? ring0 : ring1; };
 
   const int64_t items = dkv_items(a), item = item_of_slot(blockIdx.x, items * a.B * a.Hkv);
   const int bh = (int)(item / items), in_head = (int)(item % items);
@@ -233,19 +235,20 @@ __global__ __launch_bounds__(64 * kWaves) __attribute__((amdgpu_waves_per_eu(2, 
   // the row tile that is loaded next, and the one that is worked on
   int g_in = per_head ? (int)(t_begin / per_head) : 0, i_in = i_lo + (per_head ? (int)(t_begin % per_head) : 0) * TR;
   int i_now = i_in;
-  auto issue = [&](uint8_t* s) {
+  auto issue = [&](uint8_t* s) BSA_INLINE {
     const bool any = g_in < a.group;
     const int qh = kvh * a.group + (any ? g_in : 0), rows = any ? i_hi + 1 - i_in : 0;
     lq.issue(reinterpret_cast<const char*>(static_cast<const T*>(a.q) + b * a.qs.b + qh * a.qs.h + i_in * a.qs.n), rows, s, w);
     ld.issue(reinterpret_cast<const char*>(static_cast<const T*>(a.dout) + b * a.dos.b + qh * a.dos.h + i_in * a.dos.n), rows,
              s + kTile, w);
-    const int l = lane_now();
-    const uint32_t stat_off = (uint32_t)(l & 31) * 4 + (l >> 5) * (uint32_t)(a.stat_rows * 4);
+    const uint32_t stat_off = (uint32_t)lane_now() * 4;
     const float* st = a.stats + ((int64_t)b * a.H + qh) * 2 * a.stat_rows + i_in;
     const __amdgpu_buffer_rsrc_t rsrc = __builtin_amdgcn_make_buffer_rsrc(
         const_cast<float*>(st), 0, any ? (int)((a.stat_rows + TR) * 4) : 0, 0x00020000);
     __builtin_amdgcn_raw_ptr_buffer_load_lds(
         rsrc, (__attribute__((address_space(3))) void*)(s + 2 * kTile + w * kStat), 4, stat_off, 0, 0, 0);
+    __builtin_amdgcn_raw_ptr_buffer_load_lds(
+        rsrc, (__attribute__((address_space(3))) void*)(s + 2 * kTile + w * kStat + 256), 4, stat_off, (int)(a.stat_rows * 4), 0, 0);
     i_in += TR;
     if (i_in > i_hi) {
       i_in = i_lo;
@@ -272,30 +275,33 @@ __global__ __launch_bounds__(64 * kWaves) __attribute__((amdgpu_waves_per_eu(2, 
     for (int s = 0; s < kStages - 1; ++s) issue(slot(s));
   }
   for (int tb = 0; tb < nt; tb += kStages) {
-#pragma unroll
-    for (int u = 0; u < kStages; ++u) {
+    each_slot<kStages>([&](auto at) BSA_INLINE -> bool {
+      constexpr int u = decltype(at)::value;
       const int t = tb + u;
-      if (t >= nt) break;
+      if (t >= nt) return false;
       wait_vm_lgkm<(kStages - 2) * kGroup>();
       block_sync();
       issue(slot((u + kStages - 1) % kStages));
-      const uint8_t* qs = slot(u);
+      auto half = [&](auto blk) BSA_INLINE {
+      constexpr int rb = decltype(blk)::value;
+      const int i_blk = i_now + 32 * rb;
+      const uint8_t* qs = slot(u) + rb * 32 * R::kBytes;
       const uint8_t* gs = qs + kTile;
       int ro = roff, t0 = toff0, t1 = toff1;
       asm volatile("" : "+v"(ro), "+v"(t0), "+v"(t1));  // formed again per tile: sixteen addresses would not fit
-      const uint8_t* st = qs + 2 * kTile + w * kStat + 16 * (lane_now() >> 5);
+      const uint8_t* st = slot(u) + 2 * kTile + w * kStat + 128 * rb + 16 * (lane_now() >> 5);
       f32x16 s = {}, dp = {};
 #pragma unroll
       for (int c = 0; c < R::kSteps; ++c) {
         s = E::mfma(*reinterpret_cast<const x8*>(qs + (ro ^ (c << 5))), kf[c], s);
         dp = E::mfma(*reinterpret_cast<const x8*>(gs + (ro ^ (c << 5))), vf[c], dp);
       }
-      const bool full = i_now >= full_lo && i_now + TR - 1 <= full_hi;
+      const bool full = i_blk >= full_lo && i_blk + 31 <= full_hi;
       float pv[16], ds[16];
 #pragma unroll
       for (int r4 = 0; r4 < 4; ++r4) {
         const f32x4 lse = *reinterpret_cast<const f32x4*>(st + 32 * r4);
-        const f32x4 delta = *reinterpret_cast<const f32x4*>(st + 128 + 32 * r4);
+        const f32x4 delta = *reinterpret_cast<const f32x4*>(st + 256 + 32 * r4);
 #pragma unroll
         for (int e = 0; e < 4; ++e) {
           const int i = 4 * r4 + e;
@@ -307,7 +313,7 @@ __global__ __launch_bounds__(64 * kWaves) __attribute__((amdgpu_waves_per_eu(2, 
       if (__builtin_expect(!full, 0)) {
         const int l = lane_now(), key = kw + (l & 31);
         const uint32_t bits =
-            (bits_below(seen.last(key) - i_now + 1) & ~bits_below(seen.first(key) - i_now)) >> (4 * (l >> 5));
+            (bits_below(seen.last(key) - i_blk + 1) & ~bits_below(seen.first(key) - i_blk)) >> (4 * (l >> 5));
 #pragma unroll
         for (int i = 0; i < 16; ++i) {
           const bool see = (bits >> (8 * (i >> 2) + (i & 3))) & 1u;
@@ -330,9 +336,13 @@ __global__ __launch_bounds__(64 * kWaves) __attribute__((amdgpu_waves_per_eu(2, 
           dk[d] = E::mfma(read_tr_pair<T>(qs + o0, qs + o1), __builtin_bit_cast(x8, q[c]), dk[d]);
         }
       }
+      };
+      half(std::integral_constant<int, 0>{});
+      half(std::integral_constant<int, 1>{});
       i_now += TR;
       if (i_now > i_hi) i_now = i_lo;
-    }
+      return true;
+    });
   }
   wait_vm_lgkm<0>();
   const int end_lane = lane_now(), key = kw + (end_lane & 31), hh = end_lane >> 5;

@@ -205,7 +205,9 @@ template <int D>
 constexpr int kTileKeys = 4096 / D;  // 8 KB of K: 32 keys of 128 elements, 64 of 64
 
 // The keys of one row tile as a list of tiles: `ns` tiles of sinks from key 0, then
-// tiles from key w0 on.
+// tiles from key w0 on.  Keys that no row of the tile sees are in none: rows from
+// limit() on are not loaded, and a tile of sinks masks from there, since the window may
+// begin in it.
 struct KeyTiles {
   int ns, nt, w0, sink_end, end;
   template <int TK>
@@ -215,7 +217,7 @@ struct KeyTiles {
     sink_end = min(a.sinks, min(lo, end));
     ns = (sink_end + TK - 1) / TK;
     w0 = lo;
-    if (ns * TK >= lo) {  // the sinks reach the window: one range
+    if (sink_end >= lo) {  // the sinks reach the window: one range
       ns = 0;
       w0 = 0;
     }

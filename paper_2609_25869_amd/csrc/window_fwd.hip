@@ -174,11 +174,12 @@ __global__ __launch_bounds__(64 * NW) void window_fwd_kernel(WindowArgs a) {
         for (int c = 0; c < R::kSteps; ++c)
           s[kb2] = E::mfma(*reinterpret_cast<const x8*>(ks + kb2 * 32 * R::kBytes + koff[c]), qf[c], s[kb2]);
       }
-      const bool full = (j0 >= full_lo || j0 + TK <= a.sinks) && j0 + TK - 1 <= full_hi;
+      const int last = kt.limit(t) - 1;
+      const bool full = (j0 >= full_lo || j0 + TK <= a.sinks) && j0 + TK - 1 <= min(full_hi, last);
       if (!full) {
 #pragma unroll
         for (int kb2 = 0; kb2 < kNKB; ++kb2) {
-          const uint32_t bits = visible_bits(j0 + 32 * kb2, lo, hi, a.sinks) >> (4 * hh);
+          const uint32_t bits = visible_bits(j0 + 32 * kb2, lo, min(hi, last), a.sinks) >> (4 * hh);
 #pragma unroll
           for (int i = 0; i < 16; ++i) s[kb2][i] = (bits >> ((i >> 2) * 8 + (i & 3))) & 1u ? s[kb2][i] : kNegInf;
         }
@@ -306,8 +307,9 @@ void window_fwd_piped_kernel(WindowArgs a) {
   const int wave_last = min(rw + 31, nrows - 1);
   const int full_lo = wave_last >= rw ? sq.lo(a, wave_last / a.group) : kFar;
   const int full_hi = wave_last >= rw ? sq.hi(a, rw / a.group) : -1;
-  auto all_seen = [&](int j0) BSA_INLINE -> bool {
-    return (j0 >= full_lo || j0 + TK <= a.sinks) && j0 + TK - 1 <= full_hi;
+  auto all_seen = [&](int t) BSA_INLINE -> bool {
+    const int j0 = kt.key<TK>(t);
+    return (j0 >= full_lo || j0 + TK <= a.sinks) && j0 + TK - 1 <= min(full_hi, kt.limit(t) - 1);
   };
 
   Load lk, lv;
@@ -355,10 +357,11 @@ void window_fwd_piped_kernel(WindowArgs a) {
   constexpr float kSumMax = 256.f;
   const float c_log2 = a.scale_log2;
 
-  auto apply_mask = [&](f32x16* s, int j0) BSA_INLINE {
+  auto apply_mask = [&](f32x16* s, int t) BSA_INLINE {
+    const int j0 = kt.key<TK>(t), last = kt.limit(t) - 1;
 #pragma unroll
     for (int kb2 = 0; kb2 < kNKB; ++kb2) {
-      const uint32_t mine = visible_bits(j0 + 32 * kb2, lo, hi, a.sinks) >> (4 * hh);
+      const uint32_t mine = visible_bits(j0 + 32 * kb2, lo, min(hi, last), a.sinks) >> (4 * hh);
 #pragma unroll
       for (int i = 0; i < 16; ++i) {
         float x = s[kb2][i];
@@ -467,7 +470,7 @@ void window_fwd_piped_kernel(WindowArgs a) {
       acc = E::mfma(load_op(u, kslot(0), nullptr), qf[u / kNKB], u < kNKB ? f32x16{} : acc);
     }
     settle(sA);
-    apply_mask(sA, kt.key<TK>(t_begin));
+    apply_mask(sA, t_begin);
     wait_vm_lgkm<0>();
     block_sync();  // every wave has read slot 0 before it is refilled
   }
@@ -481,14 +484,14 @@ void window_fwd_piped_kernel(WindowArgs a) {
       u32x4* pw_cur = u == 0 ? pwA : pwB;
       float sum = iteration(s_cur, s_nxt, kslot(1 - u), vslot(1 - u), pw_cur, u == 0 ? pwB : pwA, t, kslot(u), vslot(u));
       // (the sum is >= 0 or NaN, which as an integer is above every number)
-      const int j0 = kt.key<TK>(t), j1 = kt.key<TK>(t + 1);
+      const int j0 = kt.key<TK>(t);
       const bool raise = __float_as_uint(sum) > __float_as_uint(kSumMax) ||
                          (m_run == kNegInf && j0 <= hi && (j0 + TK > lo || j0 < a.sinks));
-      if (__builtin_expect(__ballot(raise) != 0 || !all_seen(j1), 0)) {
+      if (__builtin_expect(__ballot(raise) != 0 || !all_seen(t + 1), 0)) {
         // both halves of a row take the same decision
         const float mine = raise ? 1.f : 0.f;
         sum = raise_reference(s_cur, pw_cur, mine + other_half(mine, lane) > 0.f, sum);
-        apply_mask(s_nxt, j1);
+        apply_mask(s_nxt, t + 1);
       }
       l_run += sum;
       wait_vm_lgkm<0>();
