@@ -1,10 +1,10 @@
 // Rotary positions on up to three axes.
 //
-// One thread owns one item of a token's head row - four interleaved pairs, or
+// One thread owns one item of a token's head rows - four interleaved pairs, or
 // eight pairs (i, i + P), or one pair where P is no multiple of eight - forms
 // the sines and cosines of its pairs once and turns that item in every
 // `lanes`-th head of Q and K (and copies it in V).  Consecutive threads hold
-// consecutive 16-byte items, then consecutive heads.
+// consecutive items, then consecutive heads.
 //
 // Angles are counted in turns: position * (freq / 2 pi) in 64 bits, less the
 // nearest integer, so a position of any size keeps the 2^-25 turns of the
@@ -33,15 +33,69 @@ __host__ __device__ inline int items_of(int d, int P) {
   return M == kInterleaved ? d / 8 : M == kHalf8 ? P / 8 + (d - 2 * P) / 8 : P + (d - 2 * P);
 }
 
+// One item of a head row: loaded, turned, stored.
 template <typename T, Mode M>
-__global__ __launch_bounds__(kThreads) void rope_kernel(RopeArgs a, int items, int lanes, int64_t total) {
-  const int64_t idx = (int64_t)blockIdx.x * kThreads + threadIdx.x;
-  if (idx >= total) return;
-  const int item = (int)(idx % items);
-  const int64_t rest = idx / items;
-  const int lane = (int)(rest % lanes);
-  const int64_t token = rest / lanes;
-  const int b = (int)(token / a.seq), n = (int)(token % a.seq);
+struct Item {
+  Vec8<T> v, z;  // kHalf1: element 0 alone; z: the pairs' second elements
+
+  __device__ void load(const T* x, int item, int P) {
+    if constexpr (M == kInterleaved) {
+      v = *reinterpret_cast<const Vec8<T>*>(x + 8 * item);
+    } else if constexpr (M == kHalf8) {
+      if (8 * item < P) {
+        v = *reinterpret_cast<const Vec8<T>*>(x + 8 * item);
+        z = *reinterpret_cast<const Vec8<T>*>(x + P + 8 * item);
+      } else {
+        v = *reinterpret_cast<const Vec8<T>*>(x + P + 8 * item);  // 2 P + 8 (item - P / 8)
+      }
+    } else {
+      v.e[0] = item < P ? x[item] : x[P + item];
+      if (item < P) z.e[0] = x[P + item];
+    }
+  }
+  __device__ void store(T* y, int item, int P) const {
+    if constexpr (M == kInterleaved) {
+      *reinterpret_cast<Vec8<T>*>(y + 8 * item) = v;
+    } else if constexpr (M == kHalf8) {
+      if (8 * item < P) {
+        *reinterpret_cast<Vec8<T>*>(y + 8 * item) = v;
+        *reinterpret_cast<Vec8<T>*>(y + P + 8 * item) = z;
+      } else {
+        *reinterpret_cast<Vec8<T>*>(y + P + 8 * item) = v;
+      }
+    } else {
+      y[item < P ? item : P + item] = v.e[0];
+      if (item < P) y[P + item] = z.e[0];
+    }
+  }
+  // the first n pairs of the item (elements past the pairs keep their bits)
+  __device__ void turn(const float* co, const float* si, int n) {
+    constexpr int kPairs = M == kInterleaved ? 4 : M == kHalf8 ? 8 : 1;
+#pragma unroll
+    for (int i = 0; i < kPairs; ++i) {
+      T& a = M == kInterleaved ? v.e[2 * i] : v.e[i];
+      T& b = M == kInterleaved ? v.e[2 * i + 1] : z.e[i];
+      if (i < n) {
+        const float u = (float)a, w = (float)b;
+        a = (T)(u * co[i] - w * si[i]);
+        b = (T)(u * si[i] + w * co[i]);
+      }
+    }
+  }
+};
+
+// A block holds tokens_per_block tokens: thread = (token, lane, item), item fastest.
+template <typename T, Mode M>
+__global__ __launch_bounds__(kThreads) void rope_kernel(RopeArgs a, int items, int lanes, int tokens_per_block) {
+  const int per_token = items * lanes;
+  const int in_block = threadIdx.x / per_token, rest = threadIdx.x % per_token;
+  const int item = rest % items, lane = rest / items;
+  const int64_t token = (int64_t)blockIdx.x * tokens_per_block + in_block;
+  const int64_t tokens = (int64_t)a.batch * a.seq;
+  if (in_block >= tokens_per_block || token >= tokens) return;
+  // (a 64-bit division is a hundred instructions)
+  const int b = tokens <= 0x7fffffff ? (int)token / a.seq : (int)(token / a.seq);
+  const int n = (int)(token - (int64_t)b * a.seq);
   if (a.lengths && n >= a.lengths[b]) return;
 
   constexpr int kPairs = M == kInterleaved ? 4 : M == kHalf8 ? 8 : 1;
@@ -61,13 +115,14 @@ __global__ __launch_bounds__(kThreads) void rope_kernel(RopeArgs a, int items, i
     pos[2] = w + a.origin[2];
     turned = n < a.volume;
   }
+  const int n_pairs = turned ? a.P - pair0 : 0;  // of the item: all of them where it is kPairs or more
   float co[kPairs], si[kPairs];
 #pragma unroll
   for (int i = 0; i < kPairs; ++i) {
-    const int pr = pair0 + i;
     co[i] = 1.f;
     si[i] = 0.f;
-    if (turned && pr < a.P) {
+    if (i < n_pairs) {
+      const int pr = pair0 + i;
       const int p = pr < a.end0 ? pos[0] : pr < a.end1 ? pos[1] : pos[2];
       double t = (double)p * (a.freq[pr] * kInv2Pi);
       t -= rint(t);
@@ -76,81 +131,51 @@ __global__ __launch_bounds__(kThreads) void rope_kernel(RopeArgs a, int items, i
     }
   }
 
-  const int64_t row_in_kv = n + (a.rows ? (int64_t)a.rows[b] : 0);
-  const bool kv_fits = row_in_kv >= 0 && row_in_kv < a.kv_rows;
-  const int hq = a.heads[0], hk = hq + a.heads[1], all = hk + a.heads[2];
-  for (int c = lane; c < all; c += lanes) {
-    const int t = c < hq ? 0 : c < hk ? 1 : 2;
-    if (t > 0 && !kv_fits) break;
-    const int h = c - (t == 0 ? 0 : t == 1 ? hq : hk);
-    const T* x = static_cast<const T*>(a.x[t]) + b * a.xs[t].b + h * a.xs[t].h + n * a.xs[t].n;
-    T* y = static_cast<T*>(a.y[t]) + b * a.ys[t].b + h * a.ys[t].h + (t == 0 ? n : row_in_kv) * a.ys[t].n;
-    if constexpr (M == kInterleaved) {
-      Vec8<T> v = *reinterpret_cast<const Vec8<T>*>(x + 8 * item);
-      if (t < 2) {
+  // the token's rows in one tensor: kBatch heads are loaded before the first is stored
+  auto rows_of = [&](int t, int64_t row, int pairs) {
+    const T* x = static_cast<const T*>(a.x[t]) + b * a.xs[t].b + n * a.xs[t].n;
+    T* y = static_cast<T*>(a.y[t]) + b * a.ys[t].b + row * a.ys[t].n;
+    constexpr int kBatch = sizeof(T) == 2 && M == kInterleaved ? 6 : 3;
+    for (int h0 = lane; h0 < a.heads[t]; h0 += kBatch * lanes) {
+      Item<T, M> r[kBatch];
 #pragma unroll
-        for (int i = 0; i < 4; ++i) {
-          const float u = (float)v.e[2 * i], w = (float)v.e[2 * i + 1];
-          // elements past the pairs (and unturned tokens) keep their bits: 1 and 0
-          // multiply exactly, but for infinities
-          if (pair0 + i < a.P && turned) {
-            v.e[2 * i] = (T)(u * co[i] - w * si[i]);
-            v.e[2 * i + 1] = (T)(u * si[i] + w * co[i]);
-          }
-        }
+      for (int i = 0; i < kBatch; ++i) {
+        const int h = h0 + i * lanes;
+        if (h < a.heads[t]) r[i].load(x + h * a.xs[t].h, item, a.P);
       }
-      *reinterpret_cast<Vec8<T>*>(y + 8 * item) = v;
-    } else if constexpr (M == kHalf8) {
-      if (pair0 < a.P) {
-        Vec8<T> v = *reinterpret_cast<const Vec8<T>*>(x + pair0);
-        Vec8<T> z = *reinterpret_cast<const Vec8<T>*>(x + a.P + pair0);
-        if (t < 2 && turned) {
 #pragma unroll
-          for (int i = 0; i < 8; ++i) {
-            const float u = (float)v.e[i], w = (float)z.e[i];
-            v.e[i] = (T)(u * co[i] - w * si[i]);
-            z.e[i] = (T)(u * si[i] + w * co[i]);
-          }
-        }
-        *reinterpret_cast<Vec8<T>*>(y + pair0) = v;
-        *reinterpret_cast<Vec8<T>*>(y + a.P + pair0) = z;
-      } else {
-        const int at = 2 * a.P + 8 * (item - a.P / 8);
-        *reinterpret_cast<Vec8<T>*>(y + at) = *reinterpret_cast<const Vec8<T>*>(x + at);
-      }
-    } else {
-      if (item < a.P) {
-        T v = x[item], z = x[a.P + item];
-        if (t < 2 && turned) {
-          const float u = (float)v, w = (float)z;
-          v = (T)(u * co[0] - w * si[0]);
-          z = (T)(u * si[0] + w * co[0]);
-        }
-        y[item] = v;
-        y[a.P + item] = z;
-      } else {
-        y[a.P + item] = x[a.P + item];
+      for (int i = 0; i < kBatch; ++i) {
+        const int h = h0 + i * lanes;
+        if (h >= a.heads[t]) continue;
+        r[i].turn(co, si, pairs);
+        r[i].store(y + h * a.ys[t].h, item, a.P);
       }
     }
-  }
+  };
+  rows_of(0, n, n_pairs);
+  const int64_t row = n + (a.rows ? (int64_t)a.rows[b] : 0);
+  if (row < 0 || row >= a.kv_rows) return;
+  rows_of(1, row, n_pairs);
+  rows_of(2, row, 0);
 }
 
 template <typename T, Mode M>
 hipError_t launch(const RopeArgs& a, hipStream_t s) {
   const int items = items_of<M>(a.d, a.P);
-  const int all = a.heads[0] + a.heads[1] + a.heads[2];
+  const int most = a.heads[0] > a.heads[1] ? a.heads[0] : a.heads[1];
   const int64_t tokens = (int64_t)a.batch * a.seq;
-  // Threads per token: a head each where tokens are few; with enough of them
-  // four heads side by side, so that the sines and cosines of a token are
-  // formed for a quarter of its heads each.
-  int lanes = all;
+  if (tokens == 0) return hipSuccess;
+  // Threads per token: with enough tokens to fill the card four heads side by side,
+  // so that the sines and cosines are formed for a quarter of the heads each; else as
+  // many as a block holds.
   constexpr int64_t kFill = int64_t(256) * 2048;  // threads the card holds
-  if (tokens * items * 4 >= kFill && all > 4) lanes = 4;
-  const int64_t total = tokens * items * lanes;
-  if (total == 0) return hipSuccess;
-  const int64_t blocks = (total + kThreads - 1) / kThreads;
+  int lanes = kThreads / items < 1 ? 1 : kThreads / items;
+  if (lanes > most) lanes = most;
+  if (lanes > 4 && tokens * items * 4 >= kFill) lanes = 4;
+  const int per_block = kThreads / (items * lanes);
+  const int64_t blocks = (tokens + per_block - 1) / per_block;
   if (blocks > 0x7fffffff) return hipErrorInvalidValue;
-  hipLaunchKernelGGL((rope_kernel<T, M>), dim3((unsigned)blocks), dim3(kThreads), 0, s, a, items, lanes, total);
+  hipLaunchKernelGGL((rope_kernel<T, M>), dim3((unsigned)blocks), dim3(kThreads), 0, s, a, items, lanes, per_block);
   return hipGetLastError();
 }
 

@@ -29,6 +29,7 @@ _lib = _ops_ffi.load()
 try:
     import torch
     _CODES = {torch.bfloat16: DTYPE_BF16, torch.float16: DTYPE_F16, torch.float32: DTYPE_F32}
+    _raw_stream = getattr(torch._C, "_cuda_getCurrentRawStream", None)
 except ImportError:  # the package's host functions work without it
     torch = None
 
@@ -98,7 +99,8 @@ def _on(device, stream):
 def _run(device, stream, call):
     """call(handle) with `device` and `stream` current."""
     if stream is None and torch.cuda.current_device() == device.index:
-        return call(torch.cuda.current_stream().cuda_stream)
+        # (building a Stream object to read its handle takes 2.6 us)
+        return call(_raw_stream(device.index) if _raw_stream else torch.cuda.current_stream().cuda_stream)
     with _on(device, stream) as handle:
         return call(handle)
 
