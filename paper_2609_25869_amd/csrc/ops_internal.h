@@ -68,7 +68,7 @@ struct WindowArgs {
 };
 
 // Key tiles of one key head as work items of the dK/dV kernel: the slices of the
-// tiles with sinks, then those of the others.  A tile cut into several slices has
+// tiles without sinks, then those of the others.  A tile cut into several slices has
 // partial sums in the workspace, in the order of the items.
 inline __host__ __device__ int64_t dkv_items(const WindowArgs& a) {
   return (int64_t)a.nsink * a.sink_slices + (int64_t)(a.nktiles - a.nsink) * a.slices;

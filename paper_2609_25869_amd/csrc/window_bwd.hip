@@ -119,11 +119,24 @@ __global__ __launch_bounds__(64 * kWaves) void window_dq_kernel(WindowArgs a) {
       int ro = roff, t0 = toff0, t1 = toff1;
       asm volatile("" : "+v"(ro), "+v"(t0), "+v"(t1));  // formed again per tile: sixteen addresses would not fit
       const int j0 = kt.key<TK>(t) + decltype(blk)::value * 32;
+      // operands in the order of their use: K and V in turn, then K again by columns
+      constexpr int kAhead = 3, kRowUnits = 2 * R::kSteps, kTrUnits = 2 * R::kBlocks;
+      auto load_op = [&](int i) BSA_INLINE -> x8 {
+        if (i < kRowUnits) return *reinterpret_cast<const x8*>((i % 2 ? vs : ks) + (ro ^ ((i / 2) << 5)));
+        const int j = i - kRowUnits, c = j / R::kBlocks, d = j % R::kBlocks;
+        const uint8_t* rows = ks + c * 16 * R::kBytes;
+        return read_tr_pair<T>(rows + (t0 ^ (d << 6)), rows + (t1 ^ (d << 6)));
+      };
+      x8 op[kAhead + 1];
+#pragma unroll
+      for (int i = 0; i < kAhead; ++i) op[i] = load_op(i);
       f32x16 s = {}, dp = {};
 #pragma unroll
-      for (int c = 0; c < R::kSteps; ++c) {
-        s = E::mfma(*reinterpret_cast<const x8*>(ks + (ro ^ (c << 5))), qf[c], s);
-        dp = E::mfma(*reinterpret_cast<const x8*>(vs + (ro ^ (c << 5))), df[c], dp);
+      for (int i = 0; i < kRowUnits; ++i) {
+        op[(i + kAhead) % (kAhead + 1)] = load_op(i + kAhead);
+        if (i % 2 == 0) s = E::mfma(op[i % (kAhead + 1)], qf[i / 2], s);
+        else dp = E::mfma(op[i % (kAhead + 1)], df[i / 2], dp);
+        __builtin_amdgcn_sched_barrier(0);
       }
       float ds[16];
 #pragma unroll
@@ -139,11 +152,11 @@ __global__ __launch_bounds__(64 * kWaves) void window_dq_kernel(WindowArgs a) {
 #pragma unroll
       for (int i = 0; i < 16; i += 2) p[i / 8][(i % 8) / 2] = pack2<T>(ds[i], ds[i + 1]);
 #pragma unroll
-      for (int c = 0; c < 2; ++c) {
-#pragma unroll
-        for (int d = 0; d < R::kBlocks; ++d)
-          acc[d] = E::mfma(read_tr_pair<T>(ks + c * 16 * R::kBytes + (t0 ^ (d << 6)), ks + c * 16 * R::kBytes + (t1 ^ (d << 6))),
-                           __builtin_bit_cast(x8, p[c]), acc[d]);
+      for (int i = 0; i < kTrUnits; ++i) {
+        const int u_at = kRowUnits + i, c = i / R::kBlocks, d = i % R::kBlocks;
+        if (i + kAhead < kTrUnits) op[(u_at + kAhead) % (kAhead + 1)] = load_op(u_at + kAhead);
+        acc[d] = E::mfma(op[u_at % (kAhead + 1)], __builtin_bit_cast(x8, p[c]), acc[d]);
+        __builtin_amdgcn_sched_barrier(0);
       }
       };
       half(std::integral_constant<int, 0>{});
@@ -197,9 +210,10 @@ __global__ __launch_bounds__(64 * kWaves) __attribute__((amdgpu_waves_per_eu(2, 
 
   const int64_t items = dkv_items(a), item = item_of_slot(blockIdx.x, items * a.B * a.Hkv);
   const int bh = (int)(item / items), in_head = (int)(item % items);
-  const bool sink = in_head < a.nsink * a.sink_slices;
+  const int plain = (a.nktiles - a.nsink) * a.slices;  // items of the tiles without sinks
+  const bool sink = in_head >= plain;
   const int nslice = sink ? a.sink_slices : a.slices;
-  const int in_kind = sink ? in_head : in_head - a.nsink * a.sink_slices;
+  const int in_kind = sink ? in_head - plain : in_head;
   const int tile = in_kind / nslice + (sink ? 0 : a.nsink), slice = in_kind % nslice;
   const int b = bh / a.Hkv, kvh = bh % a.Hkv;
   const Seq sq(a, b);
@@ -349,7 +363,7 @@ __global__ __launch_bounds__(64 * kWaves) __attribute__((amdgpu_waves_per_eu(2, 
   if (key >= sq.kv_len) return;
   if (nslice > 1) {
     // [slice][dK, dV][key][column]
-    const int64_t first_part = sink || a.sink_slices == 1 ? 0 : (int64_t)a.nsink * a.sink_slices;
+    const int64_t first_part = sink && a.slices > 1 ? plain : 0;
     float* part = a.part + ((int64_t)bh * dkv_parts(a) + first_part + in_kind) * (2 * TKEY * D) + (key - k0) * D;
 #pragma unroll
     for (int d = 0; d < R::kBlocks; ++d) {
@@ -386,17 +400,16 @@ __global__ __launch_bounds__(64 * kWaves) __attribute__((amdgpu_waves_per_eu(2, 
 template <typename T, int D>
 __global__ __launch_bounds__(256) void window_dkv_sum_kernel(WindowArgs a) {
   constexpr int TKEY = 32 * kWaves;
-  const int cut_sinks = a.sink_slices > 1 ? a.nsink : 0, cut = cut_sinks + (a.slices > 1 ? a.nktiles - a.nsink : 0);
+  const int cut_plain = a.slices > 1 ? a.nktiles - a.nsink : 0, cut = cut_plain + (a.sink_slices > 1 ? a.nsink : 0);
   const int bh = blockIdx.x / cut, c = blockIdx.x % cut;
-  const bool sink = c < cut_sinks;
-  const int tile = sink ? c : c - cut_sinks + a.nsink, nslice = sink ? a.sink_slices : a.slices;
+  const bool sink = c >= cut_plain;
+  const int tile = sink ? c - cut_plain : c + a.nsink, nslice = sink ? a.sink_slices : a.slices;
   const int b = bh / a.Hkv, kvh = bh % a.Hkv;
   const Seq sq(a, b);
   const int at = ((int)blockIdx.y * 256 + (int)threadIdx.x) * 4;  // in the tile's [key][column]
   const int key = tile * TKEY + at / D, col = at % D;
   if (key >= sq.kv_len) return;
-  const int64_t p0 = sink ? (int64_t)c * a.sink_slices
-                          : (int64_t)cut_sinks * a.sink_slices + (int64_t)(c - cut_sinks) * a.slices;
+  const int64_t p0 = sink ? (int64_t)cut_plain * a.slices + (int64_t)(c - cut_plain) * a.sink_slices : (int64_t)c * a.slices;
   const float* part = a.part + ((int64_t)bh * dkv_parts(a) + p0) * (2 * TKEY * D) + blockIdx.z * (TKEY * D) + at;
   f32x4 sum = {0.f, 0.f, 0.f, 0.f};
   for (int s = 0; s < nslice; ++s) sum += *reinterpret_cast<const f32x4*>(part + (int64_t)s * (2 * TKEY * D));
@@ -432,22 +445,26 @@ int64_t plan_backward(WindowArgs* a, int d) {
   a->ntiles = (int32_t)((rows + 32 * kWaves - 1) / (32 * kWaves));
   a->nktiles = (a->Nkv + kKeys - 1) / kKeys;
   a->stat_rows = ((int64_t)a->Nq + 63) / 32 * 32;
-  // Row tiles that a key tile walks.  Every query that lies behind a tile may see
-  // its sinks; others are seen from `right` before to `left` behind.
+  // Row tiles (of 64) that a key tile walks.  Every query that lies behind a tile may
+  // see its sinks; others are seen from `right` before to `left` behind.
   auto min64 = [](int64_t x, int64_t y) { return x < y ? x : y; };
   auto max64 = [](int64_t x, int64_t y) { return x > y ? x : y; };
-  const int64_t walk_sink = ((int64_t)a->Nq + 31) / 32 * a->group;
-  const int64_t walk = min64(walk_sink, ((int64_t)a->left + a->right + kKeys + 31) / 32 * a->group);
+  const int64_t walk_sink = ((int64_t)a->Nq + 63) / 64 * a->group;
+  const int64_t walk = min64(walk_sink, ((int64_t)a->left + a->right + kKeys + 63) / 64 * a->group);
   a->nsink = (int32_t)((a->sinks + kKeys - 1) / kKeys);
-  // Slices: a tile with sinks is cut to about the others' walk.  Where all that
-  // gives fewer than 512 workgroups, every tile is cut further; no slice is
-  // shorter than eight row tiles.
-  const int64_t bh = max64((int64_t)a->B * a->Hkv, 1);
-  int64_t goal = max64(walk, 8);
-  const int64_t total = bh * (a->nsink * walk_sink + (a->nktiles - a->nsink) * walk);
-  goal = max64(min64(goal, total / 512), 8);
-  a->sink_slices = (int32_t)max64(1, min64((walk_sink + goal - 1) / goal, 256));
+  // Slices.  A slice costs 128 KB (head dim 128) written and read again, and two
+  // workgroups share a CU: tiles without sinks are cut only where they are fewer than
+  // three quarters of the CUs.  Tiles with sinks are cut to the others' walk, and to a
+  // quarter of it where there are few workgroups, so that they fill the gaps behind
+  // the longer ones (they come last).  No slice is shorter than four row tiles.
+  const int64_t bh = max64((int64_t)a->B * a->Hkv, 1), plain = bh * (a->nktiles - a->nsink);
+  // (walks that span much of the sequence are of very different lengths: twice as many)
+  const int64_t want = 2 * walk > walk_sink ? 512 : 256;
+  const int64_t cut = plain > 0 && 4 * plain < 3 * want ? (want + plain - 1) / plain : 1;
+  const int64_t goal = max64((walk + cut - 1) / cut, 4);
+  const int64_t goal_sink = bh * a->nktiles < 1024 ? max64((goal + 3) / 4, 4) : goal;
   a->slices = (int32_t)max64(1, min64((walk + goal - 1) / goal, 256));
+  a->sink_slices = (int32_t)max64(1, min64((walk_sink + goal_sink - 1) / goal_sink, 256));
   return 2 * (int64_t)a->B * a->H * a->stat_rows + 32 + dkv_parts(*a) * a->B * a->Hkv * (2 * kKeys * d);
 }
 
