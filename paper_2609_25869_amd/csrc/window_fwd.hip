@@ -16,7 +16,7 @@ namespace bsa_ops {
 
 namespace {
 
-constexpr int kMaxSplit = 64;
+constexpr int kMaxSplit = 256;
 constexpr float kSlack = 8.f;
 
 // Inline asm must not read a matrix instruction's result too early: the compiler
@@ -80,7 +80,7 @@ __global__ __launch_bounds__(64 * NW) void window_fwd_kernel(WindowArgs a) {
   using E = Elem<T>;
   using R = Rows<D>;
   typedef typename E::x8 x8;
-  constexpr int TK = kTileKeys<D>, TQ = 32 * NW, kStages = 4;
+  constexpr int TK = kTileKeys<D>, TQ = 32 * NW, kStages = 2;
   constexpr int kNKB = TK / 32, kTile = TK * R::kBytes;
   static_assert(kTile == 8192, "K and V tiles are 8 KB");
   using Load = TileLoad<D, TK, NW>;
@@ -89,9 +89,7 @@ __global__ __launch_bounds__(64 * NW) void window_fwd_kernel(WindowArgs a) {
   // never alias the loads that fill another, and leaves those in flight
   __shared__ __attribute__((aligned(1024))) uint8_t ring0[2 * kTile];
   __shared__ __attribute__((aligned(1024))) uint8_t ring1[2 * kTile];
-  __shared__ __attribute__((aligned(1024))) uint8_t ring2[2 * kTile];
-  __shared__ __attribute__((aligned(1024))) uint8_t ring3[2 * kTile];
-  auto slot = [&](int i) -> uint8_t* { return i == 0 ? ring0 : i == 1 ? ring1 : i == 2 ? ring2 : ring3; };
+  auto slot = [&](int i) -> uint8_t* { return i == 0 ? ring0 : ring1; };
 
   const int64_t item = item_of_slot(blockIdx.x, (int64_t)a.ntiles * a.nsplit * a.B * a.Hkv);
   const int split = (int)(item % a.nsplit);
@@ -513,55 +511,70 @@ void window_fwd_piped_kernel(WindowArgs a) {
 #endif
 }
 
-// Joins the slices of a row: one wave per row, lane s holding the maximum and the
-// sum of slice s, then D / 4 lanes per slice adding up O.
-template <typename T, int D>
+// Joins the slices of a row: W waves per row, D / 4 threads a slice, with the loads of
+// four slices in flight per thread.  One wave does for eight slices; more are shared by
+// the four waves of a workgroup (65536 keys in 512 slices: 37 us with a wave per row, 32
+// with four; 2048 rows of two slices: 27 us with a wave per row, 29 with four).
+template <typename T, int D, int W>
 __global__ __launch_bounds__(256) void window_join_kernel(WindowArgs a) {
-  const int lane = threadIdx.x & 63;
+  constexpr int kCols = D / 4, kPar = 64 * W / kCols, kBatch = 4;
+  __shared__ f32x4 red[W][kCols];
+  const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6;
   const int per = a.Nq * a.group;
   const int64_t rows = (int64_t)a.B * a.Hkv * per;
-  const int64_t r = (int64_t)blockIdx.x * 4 + (threadIdx.x >> 6);
+  const int64_t r = (int64_t)blockIdx.x * (4 / W) + (W == 1 ? wave : 0);
   if (r >= rows) return;
   const int bh = (int)(r / per), row = (int)(r % per);
   const int b = bh / a.Hkv, kvh = bh % a.Hkv;
   const Seq sq(a, b);
   if (row >= sq.q_len * a.group) return;
   const float* ml = a.part + rows * a.nsplit * D + 2 * (r * a.nsplit);
-  float m = kNegInf, l = 0.f;
-  if (lane < a.nsplit) {
-    m = ml[2 * lane];
-    l = ml[2 * lane + 1];
-  }
-  float top = m;
+  // every wave forms the common maximum and sum for itself
+  float top = kNegInf, sum = 0.f;
+  for (int s = lane; s < a.nsplit; s += 64) top = fmaxf(top, ml[2 * s]);
 #pragma unroll
   for (int x = 32; x; x >>= 1) top = fmaxf(top, __shfl_xor(top, x));
-  const float wgt = m == kNegInf ? 0.f : fast_exp2(m - top);
-  float sum = wgt * l;
+  auto weight = [&](float m) { return m == kNegInf ? 0.f : fast_exp2(m - top); };
+  for (int s = lane; s < a.nsplit; s += 64) sum += weight(ml[2 * s]) * ml[2 * s + 1];
 #pragma unroll
   for (int x = 32; x; x >>= 1) sum += __shfl_xor(sum, x);
-  constexpr int kCols = D / 4, kPar = 64 / kCols;
-  const int col = (lane % kCols) * 4;
-  const float* po = a.part + r * a.nsplit * D + col;
+  const int in_row = W == 1 ? lane : tid, par = in_row / kCols, col = in_row % kCols;
+  const float* po = a.part + r * a.nsplit * D + 4 * col;
   f32x4 acc = {0.f, 0.f, 0.f, 0.f};
-  for (int s0 = 0; s0 < a.nsplit; s0 += kPar) {
-    const int s = s0 + lane / kCols;
-    const float f = __shfl(wgt, s & 63);
-    if (s < a.nsplit && f != 0.f) acc += f * *reinterpret_cast<const f32x4*>(po + (int64_t)s * D);
+  for (int s0 = par; s0 < a.nsplit; s0 += kBatch * kPar) {
+    f32x4 v[kBatch];
+    float f[kBatch];
+#pragma unroll
+    for (int i = 0; i < kBatch; ++i) {
+      const int s = s0 + i * kPar;
+      f[i] = 0.f;
+      if (s < a.nsplit) {
+        f[i] = weight(ml[2 * s]);
+        v[i] = *reinterpret_cast<const f32x4*>(po + (int64_t)s * D);
+      }
+    }
+#pragma unroll
+    for (int i = 0; i < kBatch; ++i)
+      if (f[i] != 0.f) acc += f[i] * v[i];
   }
 #pragma unroll
   for (int x = kCols; x < 64; x <<= 1) {
 #pragma unroll
     for (int e = 0; e < 4; ++e) acc[e] += __shfl_xor(acc[e], x);
   }
+  if constexpr (W > 1) {
+    if (lane < kCols) red[wave][col] = acc;
+    __syncthreads();
+    if (wave != 0) return;
+#pragma unroll
+    for (int i = 1; i < W; ++i) acc += red[i][col];
+  }
+  if (lane >= kCols) return;
   const float inv = sum > 0.f ? 1.f / sum : 0.f;
   const int qi = row / a.group, qh = kvh * a.group + row % a.group;
-  if (lane < kCols) {
-    u32x2 v;
-    v[0] = pack2<T>(acc[0] * inv, acc[1] * inv);
-    v[1] = pack2<T>(acc[2] * inv, acc[3] * inv);
-    *reinterpret_cast<u32x2*>(static_cast<T*>(a.o) + b * a.os.b + qh * a.os.h + qi * a.os.n + col) = v;
-  }
-  if (a.lse && lane == 0)
+  const u32x2 v = {pack2<T>(acc[0] * inv, acc[1] * inv), pack2<T>(acc[2] * inv, acc[3] * inv)};
+  *reinterpret_cast<u32x2*>(static_cast<T*>(a.o) + b * a.os.b + qh * a.os.h + qi * a.os.n + 4 * col) = v;
+  if (a.lse && col == 0)
     a.lse[((int64_t)b * a.H + qh) * a.Nq + qi] = sum > 0.f ? (top + __log2f(sum)) * kLn2 : kNegInf;
 }
 
@@ -579,27 +592,34 @@ hipError_t launch(const WindowArgs& a, const ForwardPlan& p, hipStream_t s) {
   hipError_t e = hipGetLastError();
   if (e != hipSuccess || p.nsplit == 1) return e;
   const int64_t rows = (int64_t)a.B * a.Hkv * a.Nq * a.group;
-  hipLaunchKernelGGL((window_join_kernel<T, D>), dim3((unsigned)((rows + 3) / 4)), dim3(256), 0, s, a);
+  if (p.nsplit <= 8) hipLaunchKernelGGL((window_join_kernel<T, D, 1>), dim3((unsigned)((rows + 3) / 4)), dim3(256), 0, s, a);
+  else hipLaunchKernelGGL((window_join_kernel<T, D, 4>), dim3((unsigned)rows), dim3(256), 0, s, a);
   return hipGetLastError();
 }
 
 }  // namespace
 
 // A row tile of 32 rows (one wave) where no key head has more, else of 128 (four
-// waves that share every K and V tile).  Where that gives too few workgroups for
-// the card, each row tile's keys are cut into slices of at least four tiles.
+// waves that share every K and V tile).  Where that gives too few workgroups for the
+// card, each row tile's keys are cut into slices.  Five one-wave workgroups share a CU
+// (32 KB rings): 1024 of them keep memory busy, and more only cost in the join, unless
+// there are 256 without slices, which 2048 even out better (64 streams of 4096 keys, 8
+// key heads: 203 us with 1024, 195 with 2048; 8 streams: 27 and 29).  A slice of two
+// tiles is worth its part of the join where there are few (1027 keys, 8 key heads: 8.7
+// us, with four tiles 9.7), eight where there are many; the four-wave kernels' pipeline
+// takes four.
 ForwardPlan plan_forward(const WindowArgs& a, int d) {
   ForwardPlan p{};
   const int64_t rows = (int64_t)a.Nq * a.group;
-  const int tk = 4096 / d;
   p.tile_rows = rows <= 32 ? 32 : 128;
   p.ntiles = (int32_t)((rows + p.tile_rows - 1) / p.tile_rows);
   const int64_t wgs = (int64_t)p.ntiles * a.B * a.Hkv;
-  const int64_t want = p.tile_rows == 32 ? 1024 : 512;
+  const int64_t want = p.tile_rows != 32 ? 512 : wgs < 256 ? 1024 : 2048;
+  const int64_t least = (p.tile_rows != 32 ? 4 : wgs < 256 ? 2 : 8) * (4096 / d);  // keys of a slice
   int64_t keys = (int64_t)a.left + a.right + 1 + (p.tile_rows + a.group - 1) / a.group;
   keys = keys < a.Nkv ? keys + (a.sinks < a.Nkv - keys ? a.sinks : a.Nkv - keys) : a.Nkv;
   int64_t split = wgs > 0 ? want / wgs : 1;
-  const int64_t most = (keys + 4 * tk - 1) / (4 * tk);
+  const int64_t most = (keys + least - 1) / least;
   split = split < most ? split : most;
   split = split < kMaxSplit ? split : kMaxSplit;
   p.nsplit = (int32_t)(split > 1 ? split : 1);

@@ -17,6 +17,7 @@ from __future__ import annotations
 
 import contextlib
 import ctypes
+import functools
 import math
 import struct
 from typing import Optional, Sequence, Tuple
@@ -240,11 +241,17 @@ def _lse_of(lse, dev, shape):
     return lse
 
 
-def _workspace(s, backward, workspace, device):
-    """(address, bytes, the tensor)"""
+@functools.lru_cache(maxsize=1024)
+def _need(s: bytes, backward: int) -> int:
+    """Bytes of workspace for packed shapes (a function of the sizes alone)."""
     need = ctypes.c_size_t()
     _check(_lib.bsa_window_workspace(s, backward, ctypes.byref(need)))
-    n = need.value
+    return need.value
+
+
+def _workspace(s, backward, workspace, device):
+    """(address, bytes, the tensor)"""
+    n = _need(s, backward)
     if n == 0:
         return None, 0, None
     if workspace is None:
@@ -258,10 +265,7 @@ def _workspace(s, backward, workspace, device):
 def window_workspace(q, k, v, left: int, right: int = 0, sinks: int = 0, *, backward: bool = False) -> int:
     """Bytes of device workspace that window_forward or window_backward needs for
     these tensors, for callers that pass their own."""
-    need = ctypes.c_size_t()
-    fields = _window_head(q, k, v, left, right, sinks, None)[4]
-    _check(_lib.bsa_window_workspace(_pack_window(*fields, 0, 0, 0), 1 if backward else 0, ctypes.byref(need)))
-    return need.value
+    return _need(_pack_window(*_window_head(q, k, v, left, right, sinks, None)[4], 0, 0, 0), 1 if backward else 0)
 
 
 def window_forward(q, k, v, left: int, right: int = 0, sinks: int = 0, *, scale: Optional[float] = None, q_len=None,
