@@ -35,47 +35,122 @@ __device__ inline float max3(float a, float b, float c) {
   return r;
 }
 
+// O of one row again, unnormalised, from the keys it sees alone: the wave takes them
+// four at a time, a lane D / 64 columns.  The products of a tile add 0 times V for the
+// keys that a row does not see, which is NaN where V is not finite; rows that come out
+// so are formed again here.  (A row that sees NaN in every column ends at that key.)
+template <typename T, int D, int TK>
+__device__ inline void row_alone(const WindowArgs& a, const KeyTiles& kt, int t_begin, int t_end, int b, int kvh, int qi,
+                                 int qh, int lo, int hi, float m, int lane, float* acc) {
+  constexpr int C = D / 64;
+  const T* q = static_cast<const T*>(a.q) + b * a.qs.b + qh * a.qs.h + qi * a.qs.n + C * lane;
+  const T* k = static_cast<const T*>(a.k) + b * a.ks.b + kvh * a.ks.h + C * lane;
+  const T* v = static_cast<const T*>(a.v) + b * a.vs.b + kvh * a.vs.h + C * lane;
+  float qv[C];
+#pragma unroll
+  for (int c = 0; c < C; ++c) {
+    qv[c] = (float)q[c];
+    acc[c] = 0.f;
+  }
+  for (int t = t_begin; t < t_end; ++t) {
+    const int j0 = kt.key<TK>(t), j1 = min(min(j0 + TK, kt.limit(t)), hi + 1);
+    for (int j = j0; j < j1; j += 4) {
+      float s[4], vv[4][C];
+#pragma unroll
+      for (int i = 0; i < 4; ++i) {
+        const int key = j + i;
+        s[i] = kNegInf;
+        if (key >= j1 || (key < lo && key >= a.sinks)) continue;
+        float dot = 0.f;
+#pragma unroll
+        for (int c = 0; c < C; ++c) {
+          dot += qv[c] * (float)k[key * a.ks.n + c];
+          vv[i][c] = (float)v[key * a.vs.n + c];
+        }
+#pragma unroll
+        for (int x = 32; x; x >>= 1) dot += __shfl_xor(dot, x);
+        s[i] = dot;
+      }
+#pragma unroll
+      for (int i = 0; i < 4; ++i) {
+        if (s[i] == kNegInf) continue;
+        const float p = fast_exp2(__builtin_fmaf(s[i], a.scale_log2, -m));
+#pragma unroll
+        for (int c = 0; c < C; ++c) acc[c] += p * vv[i][c];
+      }
+      if (__ballot(acc[0] == acc[0] || acc[C - 1] == acc[C - 1]) == 0) return;
+    }
+  }
+}
+
 // Ends a wave's work: O and LSE of its rows, or the state of its slice of the keys
 // for the join.
-template <typename T, int D>
-__device__ inline void store_rows(const WindowArgs& a, const f32x16* o, float m, float l, bool live, int b, int bh, int qi,
-                                  int qh, int row, int split, int lane) {
+template <typename T, int D, int TK>
+__device__ inline void store_rows(const WindowArgs& a, const KeyTiles& kt, int t_begin, int t_end, const f32x16* o, float m,
+                                  float l, bool live, int lo, int hi, int b, int bh, int qi, int qh, int row, int split,
+                                  int lane) {
   using R = Rows<D>;
+  constexpr int C = D / 64;
   const int hh = lane >> 5;
   l += other_half(l, lane);
-  if (!live) return;
-  if (a.nsplit == 1) {
-    const float inv = l > 0.f ? 1.f / l : 0.f;
-    T* op = static_cast<T*>(a.o) + b * a.os.b + qh * a.os.h + qi * a.os.n;
+  float zero = 0.f;  // NaN where a column is not finite
 #pragma unroll
-    for (int d = 0; d < R::kBlocks; ++d) {
+  for (int d = 0; d < R::kBlocks; ++d) {
 #pragma unroll
-      for (int g = 0; g < 4; ++g) {
-        u32x2 v;
-        v[0] = pack2<T>(o[d][4 * g] * inv, o[d][4 * g + 1] * inv);
-        v[1] = pack2<T>(o[d][4 * g + 2] * inv, o[d][4 * g + 3] * inv);
-        *reinterpret_cast<u32x2*>(op + d * 32 + 8 * g + 4 * hh) = v;
+    for (int i = 0; i < 16; ++i) zero = __builtin_fmaf(o[d][i], 0.f, zero);
+  }
+  // (a sum that is not finite itself says that the row saw such a key)
+  uint64_t again = __ballot(live && zero != 0.f && l < __builtin_huge_valf());
+  uint32_t redo = (uint32_t)again | (uint32_t)(again >> 32);
+  const bool mine = !((redo >> (lane & 31)) & 1u);
+  const float inv = l == 0.f ? 0.f : 1.f / l;
+  const int64_t rows = (int64_t)a.B * a.Hkv * a.Nq * a.group;
+  // state of a slice: [row][slice] of O, then of (m, l)
+  const int64_t at = ((int64_t)bh * a.Nq * a.group + row) * a.nsplit + split;
+  T* op = static_cast<T*>(a.o) + b * a.os.b + qh * a.os.h + qi * a.os.n;
+  float* po = a.part + at * D;
+  if (live) {
+    if (a.nsplit == 1) {
+#pragma unroll
+      for (int d = 0; d < R::kBlocks; ++d) {
+#pragma unroll
+        for (int g = 0; g < 4; ++g) {
+          u32x2 v;
+          v[0] = pack2<T>(o[d][4 * g] * inv, o[d][4 * g + 1] * inv);
+          v[1] = pack2<T>(o[d][4 * g + 2] * inv, o[d][4 * g + 3] * inv);
+          if (mine) *reinterpret_cast<u32x2*>(op + d * 32 + 8 * g + 4 * hh) = v;
+        }
       }
-    }
-    if (a.lse && hh == 0) a.lse[((int64_t)b * a.H + qh) * a.Nq + qi] = l > 0.f ? (m + __log2f(l)) * kLn2 : kNegInf;
-  } else {
-    // state of the slice: [row][slice] of O, then of (m, l)
-    const int64_t rows = (int64_t)a.B * a.Hkv * a.Nq * a.group;
-    const int64_t at = ((int64_t)bh * a.Nq * a.group + row) * a.nsplit + split;
-    float* po = a.part + at * D;
+      if (a.lse && hh == 0) a.lse[((int64_t)b * a.H + qh) * a.Nq + qi] = l == 0.f ? kNegInf : (m + __log2f(l)) * kLn2;
+    } else {
 #pragma unroll
-    for (int d = 0; d < R::kBlocks; ++d) {
+      for (int d = 0; d < R::kBlocks; ++d) {
 #pragma unroll
-      for (int g = 0; g < 4; ++g)
-        *reinterpret_cast<f32x4*>(po + d * 32 + 8 * g + 4 * hh) =
-            f32x4{o[d][4 * g], o[d][4 * g + 1], o[d][4 * g + 2], o[d][4 * g + 3]};
+        for (int g = 0; g < 4; ++g)
+          if (mine)
+            *reinterpret_cast<f32x4*>(po + d * 32 + 8 * g + 4 * hh) =
+                f32x4{o[d][4 * g], o[d][4 * g + 1], o[d][4 * g + 2], o[d][4 * g + 3]};
+      }
+      if (hh == 0) *reinterpret_cast<f32x2*>(a.part + rows * a.nsplit * D + 2 * at) = f32x2{m, l};
     }
-    if (hh == 0) *reinterpret_cast<f32x2*>(a.part + rows * a.nsplit * D + 2 * at) = f32x2{m, l};
+  }
+  for (; __builtin_expect(redo != 0, 0); redo &= redo - 1) {
+    const int r = __ffs(redo) - 1;
+    const int qi1 = __shfl(qi, r), qh1 = __shfl(qh, r), row1 = __shfl(row, r);
+    float acc[C];
+    row_alone<T, D, TK>(a, kt, t_begin, t_end, b, bh % a.Hkv, qi1, qh1, __shfl(lo, r), __shfl(hi, r), __shfl(m, r), lane, acc);
+    const float f = __shfl(inv, r);
+#pragma unroll
+    for (int c = 0; c < C; ++c) {
+      const int col = C * lane + c;
+      if (a.nsplit == 1) (static_cast<T*>(a.o) + b * a.os.b + qh1 * a.os.h + qi1 * a.os.n)[col] = (T)(acc[c] * f);
+      else a.part[(((int64_t)bh * a.Nq * a.group + row1) * a.nsplit + split) * D + col] = acc[c];
+    }
   }
 }
 
 template <typename T, int D, int NW>
-__global__ __launch_bounds__(64 * NW) void window_fwd_kernel(WindowArgs a) {
+__global__ __launch_bounds__(64 * NW, NW == 4 ? 4 : 1) void window_fwd_kernel(WindowArgs a) {
 #ifdef __HIP_DEVICE_COMPILE__
   using E = Elem<T>;
   using R = Rows<D>;
@@ -225,7 +300,7 @@ __global__ __launch_bounds__(64 * NW) void window_fwd_kernel(WindowArgs a) {
   }
   wait_vm_lgkm<0>();  // no load may still write LDS when the workgroup ends
 
-  store_rows<T, D>(a, o, m, l, live, b, bh, qi, qh, row, split, lane);
+  store_rows<T, D, TK>(a, kt, t_begin, t_end, o, m, l, live, lo, hi, b, bh, qi, qh, row, split, lane_now());
 #endif
 }
 
@@ -507,7 +582,7 @@ void window_fwd_piped_kernel(WindowArgs a) {
       o[j % R::kBlocks] = E::mfma(load_op(kNA + j, nullptr, vs), __builtin_bit_cast(x8, pw_last[j / R::kBlocks]), o[j % R::kBlocks]);
   }
   wait_vm_lgkm<0>();  // no load may still write LDS when the workgroup ends
-  store_rows<T, D>(a, o, m_run, l_run, live, b, bh, qi, qh, row, split, lane);
+  store_rows<T, D, TK>(a, kt, t_begin, t_end, o, m_run, l_run, live, lo, hi, b, bh, qi, qh, row, split, lane_now());
 #endif
 }
 
@@ -534,7 +609,7 @@ __global__ __launch_bounds__(256) void window_join_kernel(WindowArgs a) {
   for (int s = lane; s < a.nsplit; s += 64) top = fmaxf(top, ml[2 * s]);
 #pragma unroll
   for (int x = 32; x; x >>= 1) top = fmaxf(top, __shfl_xor(top, x));
-  auto weight = [&](float m) { return m == kNegInf ? 0.f : fast_exp2(m - top); };
+  auto weight = [&](float m) { return m == kNegInf ? 0.f : fast_exp2(m - top); };  // (NaN where top is infinite)
   for (int s = lane; s < a.nsplit; s += 64) sum += weight(ml[2 * s]) * ml[2 * s + 1];
 #pragma unroll
   for (int x = 32; x; x >>= 1) sum += __shfl_xor(sum, x);
@@ -570,12 +645,12 @@ __global__ __launch_bounds__(256) void window_join_kernel(WindowArgs a) {
     for (int i = 1; i < W; ++i) acc += red[i][col];
   }
   if (lane >= kCols) return;
-  const float inv = sum > 0.f ? 1.f / sum : 0.f;
+  const float inv = sum == 0.f ? 0.f : 1.f / sum;
   const int qi = row / a.group, qh = kvh * a.group + row % a.group;
   const u32x2 v = {pack2<T>(acc[0] * inv, acc[1] * inv), pack2<T>(acc[2] * inv, acc[3] * inv)};
   *reinterpret_cast<u32x2*>(static_cast<T*>(a.o) + b * a.os.b + qh * a.os.h + qi * a.os.n + 4 * col) = v;
   if (a.lse && col == 0)
-    a.lse[((int64_t)b * a.H + qh) * a.Nq + qi] = sum > 0.f ? (top + __log2f(sum)) * kLn2 : kNegInf;
+    a.lse[((int64_t)b * a.H + qh) * a.Nq + qi] = sum == 0.f ? kNegInf : (top + __log2f(sum)) * kLn2;
 }
 
 template <typename T, int D>

@@ -175,6 +175,46 @@ def test_unseen_memory_does_not_matter(case):
     check_backward(dq, dk, dv, r, "bf16", case)
 
 
+@pytest.mark.parametrize("dtype", ["bf16", "f16"])
+@pytest.mark.parametrize("case", ["square_window", "both_sides", "drafted", "ragged_f", "sinks_wide", "one_token_long_split",
+                                  "many_rows_all_keys"])
+def test_keys_that_are_not_finite_stay_with_their_queries(case, dtype):
+    """NaN in a key and infinities in a value: queries that do not see them get what
+    they get without, those that do get no number."""
+    import torch
+    x, lens, win, clipped = make(case, dtype, seed=8)
+    B, Nq = x["q"].shape[:2]
+    Nkv, Hkv = x["k"].shape[1:3]
+    kv = [clipped["kv_len"][b] if clipped["kv_len"] else Nkv for b in range(B)]
+    bad = [sorted({n // 2, n // 2 + 3, max(n - 40, 0)}) for n in kv]
+    clean = {n: t.clone() for n, t in x.items()}
+    for b in range(B):
+        for i, j in enumerate(j for j in bad[b] if j < kv[b]):
+            for t in (x, clean):
+                t["k"][b, j] *= 0.5
+            if i == 0:
+                x["k"][b, j, :, 5] = float("nan")
+            elif i == 1:
+                x["v"][b, j, :, 7] = float("inf")
+            else:
+                x["v"][b, j] = -float("inf")
+    r = expect(clean, win, clipped)
+    o, lse, *_ = sentinels(x)
+    bsa.window_forward(x["q"], x["k"], x["v"], *win, o=o, lse=lse, **lens)
+    torch.cuda.synchronize()
+    got, u, st, e = f64(o), U[dtype], STEP[dtype], r["err"]
+    hit = 0
+    for b in range(B):
+        ql = clipped["q_len"][b] if clipped["q_len"] else Nq
+        sees = owin.mask_of(ql, kv[b], ql, kv[b], *win)[:, [j for j in bad[b] if j < kv[b]]].any(1)
+        free = np.nonzero(~sees)[0]
+        tol = (1.01 * u * (e["o_u"] + np.abs(r["o"])) + st * e["o_s"] + F * e["o_u"])[b, free]
+        assert np.all(np.abs(got[b, free] - r["o"][b, free]) <= tol), "query that sees no such key"
+        assert not np.isfinite(got[b, :ql][sees]).all(-1).any(), "query that sees one"
+        hit += int(sees.sum())
+    assert hit > 0
+
+
 @pytest.mark.parametrize("layout", ["bhnd", "qkv", "broadcast", "odd_strides"])
 def test_strides(layout):
     import torch
