@@ -61,7 +61,7 @@ struct WindowArgs {
   void* dv;
   Strides dos, dqs, dks, dvs;
   float* stats;        // [B, H, 2, stat_rows]: base-2 LSE, and row sums of dO * O
-  int64_t stat_rows;   // at least Nq + 31: whole tiles of rows may be read
+  int64_t stat_rows;   // at least Nq + 63: whole tiles of rows may be read
   // dK/dV: key tiles per key head, those that hold sinks (the first ones), and the
   // slices that the queries of a tile with and without sinks are cut into
   int32_t nktiles, nsink, sink_slices, slices;

@@ -14,7 +14,17 @@
 //
 // In both a wave holds 32 of its own rows (queries, or keys) as operands in
 // registers, and the products over the head dim come out with one of those per
-// lane, which is the layout that the products over the walked rows need.
+// lane, which is the layout that the products over the walked rows need.  Two
+// workgroups of four waves share a CU; walked rows come in tiles of 64 through two
+// ring slots (with 32 and four slots, twice the barriers: dK/dV 6.9 ms for 6.3).
+//
+// P, and dS after its subtraction, are rounded to the tensors' type for the products
+// (float16 holds dS below 2^-14 to 2^-25: scale the loss where gradients are that
+// small); everything else is 32 bits.
+//
+// 28800 queries and keys, 24 heads, 7201 keys around each and 3600 sinks: dQ 4.4 ms
+// (1160 TFLOP/s of its three products), dK/dV 6.3 ms (1090 of its four), where a large
+// library product reaches 1381.
 #include "window_common.h"
 
 // (Kernel bodies are kept from the host's pass, which drops the launch stub of a
@@ -114,50 +124,50 @@ __global__ __launch_bounds__(64 * kWaves) void window_dq_kernel(WindowArgs a) {
       block_sync();
       issue(t + kStages - 1, slot((u + kStages - 1) % kStages));
       auto half = [&](auto blk) BSA_INLINE {
-      const uint8_t* ks = slot(u) + decltype(blk)::value * 32 * R::kBytes;
-      const uint8_t* vs = ks + kTile;
-      int ro = roff, t0 = toff0, t1 = toff1;
-      asm volatile("" : "+v"(ro), "+v"(t0), "+v"(t1));  // formed again per tile: sixteen addresses would not fit
-      const int j0 = kt.key<TK>(t) + decltype(blk)::value * 32;
-      // operands in the order of their use: K and V in turn, then K again by columns
-      constexpr int kAhead = 3, kRowUnits = 2 * R::kSteps, kTrUnits = 2 * R::kBlocks;
-      auto load_op = [&](int i) BSA_INLINE -> x8 {
-        if (i < kRowUnits) return *reinterpret_cast<const x8*>((i % 2 ? vs : ks) + (ro ^ ((i / 2) << 5)));
-        const int j = i - kRowUnits, c = j / R::kBlocks, d = j % R::kBlocks;
-        const uint8_t* rows = ks + c * 16 * R::kBytes;
-        return read_tr_pair<T>(rows + (t0 ^ (d << 6)), rows + (t1 ^ (d << 6)));
-      };
-      x8 op[kAhead + 1];
+        const uint8_t* ks = slot(u) + decltype(blk)::value * 32 * R::kBytes;
+        const uint8_t* vs = ks + kTile;
+        int ro = roff, t0 = toff0, t1 = toff1;
+        asm volatile("" : "+v"(ro), "+v"(t0), "+v"(t1));  // formed again per tile: sixteen addresses would not fit
+        const int j0 = kt.key<TK>(t) + decltype(blk)::value * 32;
+        // operands in the order of their use: K and V in turn, then K again by columns
+        constexpr int kAhead = 3, kRowUnits = 2 * R::kSteps, kTrUnits = 2 * R::kBlocks;
+        auto load_op = [&](int i) BSA_INLINE -> x8 {
+          if (i < kRowUnits) return *reinterpret_cast<const x8*>((i % 2 ? vs : ks) + (ro ^ ((i / 2) << 5)));
+          const int j = i - kRowUnits, c = j / R::kBlocks, d = j % R::kBlocks;
+          const uint8_t* rows = ks + c * 16 * R::kBytes;
+          return read_tr_pair<T>(rows + (t0 ^ (d << 6)), rows + (t1 ^ (d << 6)));
+        };
+        x8 op[kAhead + 1];
 #pragma unroll
-      for (int i = 0; i < kAhead; ++i) op[i] = load_op(i);
-      f32x16 s = {}, dp = {};
+        for (int i = 0; i < kAhead; ++i) op[i] = load_op(i);
+        f32x16 s = {}, dp = {};
 #pragma unroll
-      for (int i = 0; i < kRowUnits; ++i) {
-        op[(i + kAhead) % (kAhead + 1)] = load_op(i + kAhead);
-        if (i % 2 == 0) s = E::mfma(op[i % (kAhead + 1)], qf[i / 2], s);
-        else dp = E::mfma(op[i % (kAhead + 1)], df[i / 2], dp);
-        __builtin_amdgcn_sched_barrier(0);
-      }
-      float ds[16];
+        for (int i = 0; i < kRowUnits; ++i) {
+          op[(i + kAhead) % (kAhead + 1)] = load_op(i + kAhead);
+          if (i % 2 == 0) s = E::mfma(op[i % (kAhead + 1)], qf[i / 2], s);
+          else dp = E::mfma(op[i % (kAhead + 1)], df[i / 2], dp);
+          __builtin_amdgcn_sched_barrier(0);
+        }
+        float ds[16];
 #pragma unroll
-      for (int i = 0; i < 16; ++i) ds[i] = fast_exp2(__builtin_fmaf(s[i], a.scale_log2, -lse)) * (dp[i] - delta);
-      const int last = kt.limit(t) - 1;
-      const bool full = (j0 >= full_lo || j0 + 32 <= a.sinks) && j0 + 31 <= min(full_hi, last);
-      if (__builtin_expect(!full, 0)) {
-        const uint32_t bits = visible_bits(j0, lo, min(hi, last), a.sinks) >> (4 * hh);
+        for (int i = 0; i < 16; ++i) ds[i] = fast_exp2(__builtin_fmaf(s[i], a.scale_log2, -lse)) * (dp[i] - delta);
+        const int last = kt.limit(t) - 1;
+        const bool full = (j0 >= full_lo || j0 + 32 <= a.sinks) && j0 + 31 <= min(full_hi, last);
+        if (__builtin_expect(!full, 0)) {
+          const uint32_t bits = visible_bits(j0, lo, min(hi, last), a.sinks) >> (4 * hh);
 #pragma unroll
-        for (int i = 0; i < 16; ++i) zero_unless(ds[i], (bits >> ((i >> 2) * 8 + (i & 3))) & 1u);
-      }
-      u32x4 p[2];
+          for (int i = 0; i < 16; ++i) zero_unless(ds[i], (bits >> ((i >> 2) * 8 + (i & 3))) & 1u);
+        }
+        u32x4 p[2];
 #pragma unroll
-      for (int i = 0; i < 16; i += 2) p[i / 8][(i % 8) / 2] = pack2<T>(ds[i], ds[i + 1]);
+        for (int i = 0; i < 16; i += 2) p[i / 8][(i % 8) / 2] = pack2<T>(ds[i], ds[i + 1]);
 #pragma unroll
-      for (int i = 0; i < kTrUnits; ++i) {
-        const int u_at = kRowUnits + i, c = i / R::kBlocks, d = i % R::kBlocks;
-        if (i + kAhead < kTrUnits) op[(u_at + kAhead) % (kAhead + 1)] = load_op(u_at + kAhead);
-        acc[d] = E::mfma(op[u_at % (kAhead + 1)], __builtin_bit_cast(x8, p[c]), acc[d]);
-        __builtin_amdgcn_sched_barrier(0);
-      }
+        for (int i = 0; i < kTrUnits; ++i) {
+          const int u_at = kRowUnits + i, c = i / R::kBlocks, d = i % R::kBlocks;
+          if (i + kAhead < kTrUnits) op[(u_at + kAhead) % (kAhead + 1)] = load_op(u_at + kAhead);
+          acc[d] = E::mfma(op[u_at % (kAhead + 1)], __builtin_bit_cast(x8, p[c]), acc[d]);
+          __builtin_amdgcn_sched_barrier(0);
+        }
       };
       half(std::integral_constant<int, 0>{});
       half(std::integral_constant<int, 1>{});
@@ -297,59 +307,59 @@ __global__ __launch_bounds__(64 * kWaves) __attribute__((amdgpu_waves_per_eu(2, 
       block_sync();
       issue(slot((u + kStages - 1) % kStages));
       auto half = [&](auto blk) BSA_INLINE {
-      constexpr int rb = decltype(blk)::value;
-      const int i_blk = i_now + 32 * rb;
-      const uint8_t* qs = slot(u) + rb * 32 * R::kBytes;
-      const uint8_t* gs = qs + kTile;
-      int ro = roff, t0 = toff0, t1 = toff1;
-      asm volatile("" : "+v"(ro), "+v"(t0), "+v"(t1));  // formed again per tile: sixteen addresses would not fit
-      const uint8_t* st = slot(u) + 2 * kTile + w * kStat + 128 * rb + 16 * (lane_now() >> 5);
-      f32x16 s = {}, dp = {};
+        constexpr int rb = decltype(blk)::value;
+        const int i_blk = i_now + 32 * rb;
+        const uint8_t* qs = slot(u) + rb * 32 * R::kBytes;
+        const uint8_t* gs = qs + kTile;
+        int ro = roff, t0 = toff0, t1 = toff1;
+        asm volatile("" : "+v"(ro), "+v"(t0), "+v"(t1));  // formed again per tile: sixteen addresses would not fit
+        const uint8_t* st = slot(u) + 2 * kTile + w * kStat + 128 * rb + 16 * (lane_now() >> 5);
+        f32x16 s = {}, dp = {};
 #pragma unroll
-      for (int c = 0; c < R::kSteps; ++c) {
-        s = E::mfma(*reinterpret_cast<const x8*>(qs + (ro ^ (c << 5))), kf[c], s);
-        dp = E::mfma(*reinterpret_cast<const x8*>(gs + (ro ^ (c << 5))), vf[c], dp);
-      }
-      const bool full = i_blk >= full_lo && i_blk + 31 <= full_hi;
-      float pv[16], ds[16];
-#pragma unroll
-      for (int r4 = 0; r4 < 4; ++r4) {
-        const f32x4 lse = *reinterpret_cast<const f32x4*>(st + 32 * r4);
-        const f32x4 delta = *reinterpret_cast<const f32x4*>(st + 256 + 32 * r4);
-#pragma unroll
-        for (int e = 0; e < 4; ++e) {
-          const int i = 4 * r4 + e;
-          pv[i] = fast_exp2(__builtin_fmaf(s[i], a.scale_log2, -lse[e]));
-          ds[i] = pv[i] * (dp[i] - delta[e]);
+        for (int c = 0; c < R::kSteps; ++c) {
+          s = E::mfma(*reinterpret_cast<const x8*>(qs + (ro ^ (c << 5))), kf[c], s);
+          dp = E::mfma(*reinterpret_cast<const x8*>(gs + (ro ^ (c << 5))), vf[c], dp);
         }
-        __builtin_amdgcn_sched_barrier(0);
-      }
-      if (__builtin_expect(!full, 0)) {
-        const int l = lane_now(), key = kw + (l & 31);
-        const uint32_t bits =
-            (bits_below(seen.last(key) - i_blk + 1) & ~bits_below(seen.first(key) - i_blk)) >> (4 * (l >> 5));
+        const bool full = i_blk >= full_lo && i_blk + 31 <= full_hi;
+        float pv[16], ds[16];
 #pragma unroll
-        for (int i = 0; i < 16; ++i) {
-          const bool see = (bits >> (8 * (i >> 2) + (i & 3))) & 1u;
-          zero_unless(pv[i], see);
-          zero_unless(ds[i], see);
+        for (int r4 = 0; r4 < 4; ++r4) {
+          const f32x4 lse = *reinterpret_cast<const f32x4*>(st + 32 * r4);
+          const f32x4 delta = *reinterpret_cast<const f32x4*>(st + 256 + 32 * r4);
+#pragma unroll
+          for (int e = 0; e < 4; ++e) {
+            const int i = 4 * r4 + e;
+            pv[i] = fast_exp2(__builtin_fmaf(s[i], a.scale_log2, -lse[e]));
+            ds[i] = pv[i] * (dp[i] - delta[e]);
+          }
+          __builtin_amdgcn_sched_barrier(0);
         }
-      }
-      u32x4 p[2], q[2];
+        if (__builtin_expect(!full, 0)) {
+          const int l = lane_now(), key = kw + (l & 31);
+          const uint32_t bits =
+              (bits_below(seen.last(key) - i_blk + 1) & ~bits_below(seen.first(key) - i_blk)) >> (4 * (l >> 5));
 #pragma unroll
-      for (int i = 0; i < 16; i += 2) {
-        p[i / 8][(i % 8) / 2] = pack2<T>(pv[i], pv[i + 1]);
-        q[i / 8][(i % 8) / 2] = pack2<T>(ds[i], ds[i + 1]);
-      }
-#pragma unroll
-      for (int c = 0; c < 2; ++c) {
-#pragma unroll
-        for (int d = 0; d < R::kBlocks; ++d) {
-          const int o0 = c * 16 * R::kBytes + (t0 ^ (d << 6)), o1 = c * 16 * R::kBytes + (t1 ^ (d << 6));
-          dv[d] = E::mfma(read_tr_pair<T>(gs + o0, gs + o1), __builtin_bit_cast(x8, p[c]), dv[d]);
-          dk[d] = E::mfma(read_tr_pair<T>(qs + o0, qs + o1), __builtin_bit_cast(x8, q[c]), dk[d]);
+          for (int i = 0; i < 16; ++i) {
+            const bool see = (bits >> (8 * (i >> 2) + (i & 3))) & 1u;
+            zero_unless(pv[i], see);
+            zero_unless(ds[i], see);
+          }
         }
-      }
+        u32x4 p[2], q[2];
+#pragma unroll
+        for (int i = 0; i < 16; i += 2) {
+          p[i / 8][(i % 8) / 2] = pack2<T>(pv[i], pv[i + 1]);
+          q[i / 8][(i % 8) / 2] = pack2<T>(ds[i], ds[i + 1]);
+        }
+#pragma unroll
+        for (int c = 0; c < 2; ++c) {
+#pragma unroll
+          for (int d = 0; d < R::kBlocks; ++d) {
+            const int o0 = c * 16 * R::kBytes + (t0 ^ (d << 6)), o1 = c * 16 * R::kBytes + (t1 ^ (d << 6));
+            dv[d] = E::mfma(read_tr_pair<T>(gs + o0, gs + o1), __builtin_bit_cast(x8, p[c]), dv[d]);
+            dk[d] = E::mfma(read_tr_pair<T>(qs + o0, qs + o1), __builtin_bit_cast(x8, q[c]), dk[d]);
+          }
+        }
       };
       half(std::integral_constant<int, 0>{});
       half(std::integral_constant<int, 1>{});
@@ -444,7 +454,7 @@ int64_t plan_backward(WindowArgs* a, int d) {
   const int64_t rows = (int64_t)a->Nq * a->group;
   a->ntiles = (int32_t)((rows + 32 * kWaves - 1) / (32 * kWaves));
   a->nktiles = (a->Nkv + kKeys - 1) / kKeys;
-  a->stat_rows = ((int64_t)a->Nq + 63) / 32 * 32;
+  a->stat_rows = ((int64_t)a->Nq + 127) / 64 * 64;  // whole tiles of 64 rows may be read
   // Row tiles (of 64) that a key tile walks.  Every query that lies behind a tile may
   // see its sinks; others are seen from `right` before to `left` behind.
   auto min64 = [](int64_t x, int64_t y) { return x < y ? x : y; };
@@ -465,13 +475,13 @@ int64_t plan_backward(WindowArgs* a, int d) {
   const int64_t goal_sink = bh * a->nktiles < 1024 ? max64((goal + 3) / 4, 4) : goal;
   a->slices = (int32_t)max64(1, min64((walk + goal - 1) / goal, 256));
   a->sink_slices = (int32_t)max64(1, min64((walk_sink + goal_sink - 1) / goal_sink, 256));
-  return 2 * (int64_t)a->B * a->H * a->stat_rows + 32 + dkv_parts(*a) * a->B * a->Hkv * (2 * kKeys * d);
+  return 2 * (int64_t)a->B * a->H * a->stat_rows + dkv_parts(*a) * a->B * a->Hkv * (2 * kKeys * d);
 }
 
 hipError_t launch_window_backward(int dtype, int d, const WindowArgs& args, hipStream_t s) {
   WindowArgs a = args;
   plan_backward(&a, d);
-  a.part = a.stats + 2 * (int64_t)a.B * a.H * a.stat_rows + 32;
+  a.part = a.stats + 2 * (int64_t)a.B * a.H * a.stat_rows;
   if (dtype == kBf16) return d == 128 ? launch<__bf16, 128>(a, s) : launch<__bf16, 64>(a, s);
   return d == 128 ? launch<_Float16, 128>(a, s) : launch<_Float16, 64>(a, s);
 }

@@ -238,9 +238,10 @@ __device__ inline int lane_now() {
 
 // x = keep ? x : 0 in place (keep is per lane), in a branch that is rarely taken: the
 // tied operand pins the result to its register, and the compiler cannot turn the
-// branch into selections that run every time.
+// branch into selections that run every time.  (The condition may have been written by
+// the instruction before: the compiler adds no wait states for inline asm.)
 __device__ inline void zero_unless(float& x, bool keep) {
-  asm volatile("v_cndmask_b32_e64 %0, 0, %0, %1" : "+v"(x) : "s"(__ballot(keep)));
+  asm volatile("s_nop 1\n\tv_cndmask_b32_e64 %0, 0, %0, %1" : "+v"(x) : "s"(__ballot(keep)));
 }
 
 // Dispatch order: the eight XCDs take consecutive workgroups in turn, so slot s

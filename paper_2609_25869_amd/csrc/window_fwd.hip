@@ -306,10 +306,11 @@ __global__ __launch_bounds__(64 * NW, NW == 4 ? 4 : 1) void window_fwd_kernel(Wi
 
 // x = keep ? x : -inf, in place (keep is per lane).  The tied operand pins the
 // result to its register: written plainly, the compiler copies the scores on the
-// common path, where nothing is masked.
+// common path, where nothing is masked.  (The condition may have been written by the
+// instruction before: the compiler adds no wait states for inline asm.)
 __device__ inline void mask_inplace(float& x, bool keep) {
   const float ninf = kNegInf;
-  asm volatile("v_cndmask_b32_e64 %0, %1, %0, %2" : "+v"(x) : "v"(ninf), "s"(__ballot(keep)));
+  asm volatile("s_nop 1\n\tv_cndmask_b32_e64 %0, %1, %0, %2" : "+v"(x) : "v"(ninf), "s"(__ballot(keep)));
 }
 
 // The kernel for 128-row tiles of head dim 128: four waves of 32 rows, tiles of 64

@@ -75,6 +75,25 @@ def test_build_options():
         assert not {"-ffast-math", "-Ofast", "-fno-honor-nans", "-ffinite-math-only"} & set(flags)
 
 
+@pytest.mark.parametrize("src,least", [("window_fwd.hip", 14), ("window_bwd.hip", 12), ("rope.hip", 9)])
+def test_kernels_keep_their_state_in_registers(tmp_path, src, least):
+    b = _builder()
+    try:
+        cc = b.hipcc()
+    except RuntimeError:
+        pytest.skip("hipcc not available")
+    out = str(tmp_path / "k.s")
+    subprocess.check_call([cc] + b.common_flags() + b.EXTRA_FLAGS.get(src, []) +
+                          ["--offload-device-only", "-S", os.path.join(b.CSRC, src), "-o", out],
+                          stderr=subprocess.DEVNULL)
+    text = open(out).read()
+    text = text[text.index("amdhsa.kernels:"):]
+    kernels = [n for n in re.findall(r"\.name:\s+(\S+)", text) if "kernel" in n]
+    sizes = [int(x) for x in re.findall(r"\.private_segment_fixed_size:\s+(\d+)", text)]
+    assert len(kernels) == len(sizes) >= least
+    assert not any(sizes), dict(zip(kernels, sizes))
+
+
 def contiguous(n, h, d):
     return (ctypes.c_int64 * 3)(n * h * d, d, h * d)
 
