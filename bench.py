@@ -164,6 +164,9 @@ def main():
     ap.add_argument("--sparsify", action="store_true",
                     help="top-k workloads: build the mask on the device inside every request "
                          "(bsa_sparsify_topk -> bsa_plan -> bsa_forward) instead of reading a resident one")
+    ap.add_argument("--rope", default="", metavar="T,H,W",
+                    help="rotate Q and K by their positions on this row-major grid inside every request "
+                         "(bsa_rope -> bsa_plan -> bsa_forward); resident masks only")
     ap.add_argument("--copy-probe", type=int, default=0, metavar="MIB",
                     help="only run a plain device copy of MIB MiB five times (HBM counter calibration) and exit")
     args = ap.parse_args()
@@ -207,6 +210,15 @@ def main():
         # the device sparsifier reproduces the workload's mask recipe; report any difference
         n_diff = int((dev_mask.cpu().numpy().reshape(-1) != mask.data.reshape(-1)).sum())
         log("device sparsifier: %d of %d mask entries differ from the workload mask" % (n_diff, mask.data.size))
+    rope = None
+    if args.rope:
+        if args.sparsify:
+            print("--rope applies to resident masks only", file=sys.stderr)
+            sys.exit(2)
+        rope_grid = tuple(int(x) for x in args.rope.split(","))
+        pairs = (d // 2 - 2 * (d // 6), d // 6, d // 6)   # time, height, width
+        rope = dict(freq=bsa.rope_frequencies(pairs), pairs=pairs, grid=rope_grid, out_q=torch.empty_like(qd),
+                    out_k=torch.empty_like(kd))
     per_head = not mask.uniform_geometry
     bq = [int(x) for x in mask.bq] if per_head else int(mask.bq[0])
     bkv = [int(x) for x in mask.bkv] if per_head else int(mask.bkv[0])
@@ -224,7 +236,17 @@ def main():
             flush.fill_(1)
         torch.cuda.synchronize()
 
+    rope_ms = []
+
     def request():
+        qr, kr = qd, kd
+        if rope is not None:
+            r0 = torch.cuda.Event(enable_timing=True)
+            r1 = torch.cuda.Event(enable_timing=True)
+            r0.record(stream)
+            qr, kr = bsa.rope(qd, kd, stream=stream, **rope)
+            r1.record(stream)
+            rope_ms.append((r0, r1))
         if topk is not None:
             s0 = torch.cuda.Event(enable_timing=True)
             s1 = torch.cuda.Event(enable_timing=True)
@@ -238,7 +260,7 @@ def main():
         e0 = torch.cuda.Event(enable_timing=True)
         e1 = torch.cuda.Event(enable_timing=True)
         e0.record(stream)
-        bsa.forward(p, qd, kd, vd, od, lse, stream=stream)
+        bsa.forward(p, qr, kr, vd, od, lse, stream=stream)
         e1.record(stream)
         return p, e0, e1
 
@@ -326,6 +348,10 @@ def main():
         sp = [a.elapsed_time(b) for a, b in sp_ms[-args.steps:]]
         out["sparsify_ms"] = {"mean": float(np.mean(sp)), "median": float(np.median(sp)), "topk": topk,
                               "in_request": True}
+    if rope is not None:
+        rp = [a.elapsed_time(b) for a, b in rope_ms[-args.steps:]]
+        out["rope_ms"] = {"mean": float(np.mean(rp)), "median": float(np.median(rp)), "grid": list(rope_grid),
+                          "in_request": True}
     # outside the timed region: the practical MFMA ceiling of this machine
     if not args.no_gemm_probe:
         probe = gemm_probe(torch)
