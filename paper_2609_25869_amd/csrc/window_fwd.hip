@@ -677,26 +677,44 @@ hipError_t launch(const WindowArgs& a, const ForwardPlan& p, hipStream_t s) {
 
 // A row tile of 32 rows (one wave) where no key head has more, else of 128 (four
 // waves that share every K and V tile).  Where that gives too few workgroups for the
-// card, each row tile's keys are cut into slices.  Five one-wave workgroups share a CU
-// (32 KB rings): 1024 of them keep memory busy, and more only cost in the join, unless
-// there are 256 without slices, which 2048 even out better (64 streams of 4096 keys, 8
-// key heads: 203 us with 1024, 195 with 2048; 8 streams: 27 and 29).  A slice of two
-// tiles is worth its part of the join where there are few (1027 keys, 8 key heads: 8.7
-// us, with four tiles 9.7), eight where there are many; the four-wave kernels' pipeline
-// takes four.
+// card, each row tile's keys are cut into slices.
+//
+// One-wave kernel: five workgroups share a CU (32 KB rings).  1024 of them keep memory
+// busy, and more only cost in the join, unless there are 256 without slices, which 2048
+// even out better (64 streams of 4096 keys, 8 key heads: 203 us with 1024, 195 with
+// 2048; 8 streams: 27 and 29).  A slice of two tiles is worth its part of the join where
+// there are few (1027 keys, 8 key heads: 8.7 us, with four tiles 9.7), eight where there
+// are many.
+//
+// Four-wave kernels: a slice's partial rows are written and read again, 66 KB each at
+// head dim 128, so slices are weighed: a tile of 64 keys takes a workgroup 1.2 us (1.74
+// with two on a CU), the join 4 us and 27 ns a slice and workgroup.  (96 row tiles of 504
+// keys: 16.5 us whole, 29.7 in five slices; 3 row tiles of 8000 keys: 65 us in two
+// slices, 20 in forty.)
 ForwardPlan plan_forward(const WindowArgs& a, int d) {
   ForwardPlan p{};
   const int64_t rows = (int64_t)a.Nq * a.group;
   p.tile_rows = rows <= 32 ? 32 : 128;
   p.ntiles = (int32_t)((rows + p.tile_rows - 1) / p.tile_rows);
   const int64_t wgs = (int64_t)p.ntiles * a.B * a.Hkv;
-  const int64_t want = p.tile_rows != 32 ? 512 : wgs < 256 ? 1024 : 2048;
-  const int64_t least = (p.tile_rows != 32 ? 4 : wgs < 256 ? 2 : 8) * (4096 / d);  // keys of a slice
   int64_t keys = (int64_t)a.left + a.right + 1 + (p.tile_rows + a.group - 1) / a.group;
   keys = keys < a.Nkv ? keys + (a.sinks < a.Nkv - keys ? a.sinks : a.Nkv - keys) : a.Nkv;
-  int64_t split = wgs > 0 ? want / wgs : 1;
-  const int64_t most = (keys + least - 1) / least;
-  split = split < most ? split : most;
+  int64_t split = 1;
+  if (p.tile_rows == 32 && wgs > 0) {
+    const int64_t least = (wgs < 256 ? 2 : 8) * (4096 / d), most = (keys + least - 1) / least;
+    split = (wgs < 256 ? 1024 : 2048) / wgs;
+    split = split < most ? split : most;
+  } else if (wgs > 0) {
+    const int64_t tiles = (keys + 63) / 64;
+    int64_t best = tiles * (wgs <= 256 ? 1200 : 1740);  // ns
+    for (int64_t s = 2; s * wgs <= 512 && s <= tiles; ++s) {
+      const int64_t t = (tiles + s - 1) / s * (s * wgs <= 256 ? 1200 : 1740) + 4000 + 27 * s * wgs * d / 128;
+      if (t < best) {
+        best = t;
+        split = s;
+      }
+    }
+  }
   split = split < kMaxSplit ? split : kMaxSplit;
   p.nsplit = (int32_t)(split > 1 ? split : 1);
   p.part_floats = p.nsplit > 1 ? (int64_t)a.B * a.Hkv * rows * p.nsplit * (d + 2) : 0;
