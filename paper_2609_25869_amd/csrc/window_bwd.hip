@@ -464,17 +464,20 @@ int64_t plan_backward(WindowArgs* a, int d) {
   a->nsink = (int32_t)((a->sinks + kKeys - 1) / kKeys);
   // Slices.  A slice costs 128 KB (head dim 128) written and read again, and two
   // workgroups share a CU: tiles without sinks are cut only where they are fewer than
-  // three quarters of the CUs.  Tiles with sinks are cut to the others' walk, and to a
-  // quarter of it where there are few workgroups, so that they fill the gaps behind
-  // the longer ones (they come last).  No slice is shorter than four row tiles.
+  // three quarters of the CUs (twice that where walks span much of the sequence, and so
+  // are of very different lengths; one key head, 4096 tokens, all keys before: 300 us with
+  // 256 workgroups, 238 with 512).  Tiles with sinks are cut to the others' walk, and to a
+  // quarter of it where there are few workgroups, so that they fill the gaps behind the
+  // longer ones (they come last).  No slice is shorter than four row tiles, and the slices
+  // of sinks take half a gigabyte at most.
   const int64_t bh = max64((int64_t)a->B * a->Hkv, 1), plain = bh * (a->nktiles - a->nsink);
-  // (walks that span much of the sequence are of very different lengths: twice as many)
   const int64_t want = 2 * walk > walk_sink ? 512 : 256;
   const int64_t cut = plain > 0 && 4 * plain < 3 * want ? (want + plain - 1) / plain : 1;
   const int64_t goal = max64((walk + cut - 1) / cut, 4);
   const int64_t goal_sink = bh * a->nktiles < 1024 ? max64((goal + 3) / 4, 4) : goal;
+  const int64_t most_sink = max64(4096 / (bh * max64(a->nsink, 1)), 1);
   a->slices = (int32_t)max64(1, min64((walk + goal - 1) / goal, 256));
-  a->sink_slices = (int32_t)max64(1, min64((walk_sink + goal_sink - 1) / goal_sink, 256));
+  a->sink_slices = (int32_t)max64(1, min64((walk_sink + goal_sink - 1) / goal_sink, min64(most_sink, 256)));
   return 2 * (int64_t)a->B * a->H * a->stat_rows + dkv_parts(*a) * a->B * a->Hkv * (2 * kKeys * d);
 }
 
