@@ -59,7 +59,7 @@ typedef struct {
   int32_t pairs[3];
   int32_t interleaved, inverse;
   int32_t grid[3], origin[3]; /* used when positions is NULL */
-  int32_t kv_rows;            /* tokens that k_out and v_out have room for */
+  int32_t kv_rows;            /* tokens that k_out and v_out have room for (seq or more without rows) */
   int64_t pos_stride[2];      /* (axis, batch), elements */
   int64_t q_stride[3], k_stride[3], v_stride[3];             /* (batch, head, token), elements */
   int64_t q_out_stride[3], k_out_stride[3], v_out_stride[3]; /* (batch, head, token), elements */
@@ -126,7 +126,10 @@ BSA_API bsa_status bsa_window_workspace(const bsa_window_shapes* shapes, int32_t
  *                  is 0), 16-byte aligned, used until the call's work is done;
  *                  calls that overlap in time need workspaces of their own.
  * dtype bf16 or f16, head_dim 64 or 128.  batch, seq_q and seq_kv may be 0.
- * Results do not depend on the order in which workgroups run.
+ * Probabilities are rounded to the tensors' type for their product with V; their
+ * sum, the maximum and O are 32 bits.  Values of K and V that are not finite
+ * reach the queries that see them and no others.  Results do not depend on the
+ * order in which workgroups run.
  */
 BSA_API bsa_status bsa_window_forward(const bsa_window_shapes* shapes, const void* q, const void* k, const void* v,
                                       void* o, float* lse, const int32_t* q_len, const int32_t* kv_len,
@@ -138,6 +141,11 @@ BSA_API bsa_status bsa_window_forward(const bsa_window_shapes* shapes, const voi
  * gradient of a key head that several query heads share is their sum.  Rows of
  * dq from q_len on and of dk and dv from kv_len on keep what they held; keys
  * that no query sees get 0.  Sums are taken in a fixed order (no atomics).
+ * Probabilities and the scores' gradients are rounded to the tensors' type for
+ * their products; float16 holds the latter to 2^-25 below 2^-14, so the loss is
+ * scaled where they are smaller.  Rows behind a sequence's end and keys that no
+ * query sees are never read, but a value that is not finite anywhere else may
+ * reach the gradients of neighbouring rows and keys that it is not visible to.
  */
 BSA_API bsa_status bsa_window_backward(const bsa_window_shapes* shapes, const bsa_window_grads* grads, const void* q,
                                        const void* k, const void* v, const void* o, const float* lse,

@@ -5,6 +5,7 @@
 #include <cmath>
 #include <cstdarg>
 #include <cstdio>
+#include <initializer_list>
 
 #include "ops_internal.h"
 
@@ -131,6 +132,13 @@ bsa_status check_workspace(int64_t need, const void* workspace, size_t bytes) {
   return BSA_OK;
 }
 
+// A result is not written over a tensor that other workgroups still read.
+bsa_status check_apart(const char* name, const void* out, std::initializer_list<const void*> inputs) {
+  for (const void* p : inputs)
+    if (out && out == p) return fail(BSA_ERR_INVALID, "%s is one of the inputs", name);
+  return BSA_OK;
+}
+
 #define TRY(x)                          \
   do {                                  \
     const bsa_status st_ = (x);         \
@@ -181,7 +189,9 @@ bsa_status bsa_rope(const bsa_rope_shapes* shapes, const double* freq, const int
   const int64_t size = elem_size(s.dtype);
   TRY(check_tensor({"q", q, s.q_stride, s.batch, s.heads, s.seq, s.head_dim, false}, size));
   TRY(check_tensor({"q_out", q_out, s.q_out_stride, s.batch, s.heads, s.seq, s.head_dim, true}, size));
-  const int64_t kv_rows = rows ? s.kv_rows : std::min(s.seq, s.kv_rows);
+  if (!rows && with_k && s.kv_rows < s.seq)
+    return fail(BSA_ERR_INVALID, "kv_rows (%d) must be seq or more where rows is NULL", s.kv_rows);
+  const int64_t kv_rows = rows ? s.kv_rows : s.seq;
   if (with_k) {
     TRY(check_tensor({"k", k, s.k_stride, s.batch, s.kv_heads, s.seq, s.head_dim, false}, size));
     TRY(check_tensor({"k_out", k_out, s.k_out_stride, s.batch, s.kv_heads, kv_rows, s.head_dim, true}, size));
@@ -259,6 +269,7 @@ bsa_status bsa_window_forward(const bsa_window_shapes* shapes, const void* q, co
   TRY(check_tensor({"v", v, s.v_stride, s.batch, s.kv_heads, s.seq_kv, s.head_dim, false}, 2));
   TRY(check_tile_stride("k", s.k_stride[2]));
   TRY(check_tile_stride("v", s.v_stride[2]));
+  TRY(check_apart("o", o, {q, k, v}));
   WindowArgs a = window_args(s);
   TRY(check_workspace(window_bytes(a, s.head_dim, false), workspace, workspace_bytes));
   a.q = q;
@@ -294,6 +305,9 @@ bsa_status bsa_window_backward(const bsa_window_shapes* shapes, const bsa_window
   TRY(check_tile_stride("dout", g.do_stride[2]));
   TRY(check_tile_stride("k", s.k_stride[2]));
   TRY(check_tile_stride("v", s.v_stride[2]));
+  TRY(check_apart("dq", dq, {q, k, v, o, dout, dk, dv}));
+  TRY(check_apart("dk", dk, {q, k, v, o, dout, dv}));
+  TRY(check_apart("dv", dv, {q, k, v, o, dout}));
   WindowArgs a = window_args(s);
   TRY(check_workspace(window_bytes(a, s.head_dim, true), workspace, workspace_bytes));
   a.q = q;

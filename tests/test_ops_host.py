@@ -114,7 +114,7 @@ def window(**kw):
 
 
 def forward(s, ptrs=None, ws=PTR, n=1 << 40):
-    p = dict(q=PTR, k=PTR, v=PTR, o=PTR, lse=PTR)
+    p = dict(q=PTR, k=PTR, v=PTR, o=2 * PTR, lse=PTR)
     p.update(ptrs or {})
     return LIB.bsa_window_forward(ctypes.byref(s) if s is not None else None, p["q"], p["k"], p["v"], p["o"], p["lse"],
                                   None, None, ws, n, None)
@@ -131,7 +131,7 @@ def grads(s, **kw):
 
 def backward(s, g, ptrs=None, ws=PTR, n=1 << 40):
     names = ("q", "k", "v", "o", "lse", "dout", "dq", "dk", "dv")
-    p = dict.fromkeys(names, PTR)
+    p = {x: PTR * (1 + i) for i, x in enumerate(names)}
     p.update(ptrs or {})
     return LIB.bsa_window_backward(ctypes.byref(s), ctypes.byref(g) if g is not None else None,
                                    *[p[x] for x in names], None, None, ws, n, None)
@@ -177,6 +177,24 @@ def test_window_pointers_and_workspace():
     assert LIB.bsa_window_workspace(ctypes.byref(window(heads=5)), 0, ctypes.byref(need)) == INVALID and need.value == 0
 
 
+def test_results_over_inputs_are_refused():
+    s = window()
+    for name in ("q", "k", "v"):
+        assert forward(s, {name: 2 * PTR}) == INVALID and "inputs" in LIB.bsa_ops_last_error().decode()
+    for out in ("dq", "dk", "dv"):
+        for name in ("q", "k", "v", "o", "dout"):
+            assert backward(s, grads(s), {out: 64 * PTR, name: 64 * PTR}) == INVALID
+            assert out in LIB.bsa_ops_last_error().decode()
+    assert backward(s, grads(s), dict(dk=64 * PTR, dv=64 * PTR)) == INVALID
+
+
+def test_workspace_of_many_sinks_is_bounded():
+    need = ctypes.c_size_t()
+    s = window(batch=1, heads=24, kv_heads=24, seq_q=115200, seq_kv=115200, left=256, sinks=3600)
+    assert LIB.bsa_window_workspace(ctypes.byref(s), 1, ctypes.byref(need)) == 0
+    assert need.value < 1 << 30
+
+
 def test_window_backward_refusals():
     s = window()
     g = grads(s)
@@ -220,7 +238,7 @@ BAD_ROPE = [
     (dict(ptrs=dict(q_out=None)), INVALID, "q_out"), (dict(ptrs=dict(k_out=None)), INVALID, "k_out"),
     (dict(ptrs=dict(v_out=PTR + 2)), INVALID, "v_out"), (dict(q_stride=(7680, 64, 257)), INVALID, "aligned"),
     (dict(k_out_stride=(0, 64, 128)), INVALID, "overlap"), (dict(seq=(1 << 29) + 1), UNSUPPORTED, "2^29"),
-    (dict(ptrs=dict(k_out=PTR), rows=PTR), INVALID, "in place"),
+    (dict(ptrs=dict(k_out=PTR), rows=PTR), INVALID, "in place"), (dict(kv_rows=29), INVALID, "kv_rows"),
     (dict(ptrs=dict(q_out=PTR), q_out_stride=(7680, 1920, 64)), INVALID, "in place"),
 ]
 
