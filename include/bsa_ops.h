@@ -75,7 +75,7 @@ typedef struct {
  *            that the new tokens are appended to); NULL means row 0.  Rows
  *            outside [0, kv_rows) are not written.
  * q_out may be q itself, and k_out k itself when rows is NULL (same strides);
- * v_out may be v itself likewise.
+ * v_out may be v itself likewise.  No tensor is the output of another.
  * dtype bf16, f16 or f32; head_dim a multiple of 8 up to 256.  k may be NULL
  * with kv_heads 0; v may be NULL.  batch and seq may be 0.
  */
@@ -127,8 +127,9 @@ BSA_API bsa_status bsa_window_workspace(const bsa_window_shapes* shapes, int32_t
  *                  calls that overlap in time need workspaces of their own.
  * dtype bf16 or f16, head_dim 64 or 128.  batch, seq_q and seq_kv may be 0.
  * Probabilities are rounded to the tensors' type for their product with V; their
- * sum, the maximum and O are 32 bits.  Values of K and V that are not finite
- * reach the queries that see them and no others.  Results do not depend on the
+ * sum, the maximum and O are 32 bits (O before its division by the sum: values
+ * of V of 2^127 / (256 kv_len) and more may overflow it).  Values of K and V
+ * that are not finite reach the queries that see them and no others.  Results do not depend on the
  * order in which workgroups run.
  */
 BSA_API bsa_status bsa_window_forward(const bsa_window_shapes* shapes, const void* q, const void* k, const void* v,

@@ -33,6 +33,9 @@ struct RopeArgs {
   const int32_t* rows;
 };
 
+// A launch counts its threads in 32 bits.
+inline bool fits_launch(int64_t blocks, int threads) { return blocks <= (int64_t)0xffffffff / threads; }
+
 hipError_t launch_rope(int dtype, bool interleaved, const RopeArgs& a, hipStream_t s);
 
 // Window attention.  A row is one query of one head; the rows of the heads that

@@ -35,6 +35,7 @@ int64_t elem_size(int32_t dtype) { return dtype == BSA_DTYPE_F32 ? 4 : 2; }
 // their differences stay within 32 bits.
 constexpr int64_t kMaxSeq = int64_t(1) << 29;
 constexpr int64_t kMaxRows = int64_t(1) << 30;
+constexpr float kLog2e = 1.44269504088896340736f;
 
 // A tensor [batch, tokens, heads, d] with strides (batch, head, token).
 struct Tensor {
@@ -82,7 +83,7 @@ bsa_status check_window(const bsa_window_shapes* sp) {
   if (s.heads % s.kv_heads) return fail(BSA_ERR_INVALID, "heads (%d) must be a multiple of kv_heads (%d)", s.heads, s.kv_heads);
   if (s.left < -1 || s.right < -1 || s.sinks < 0)
     return fail(BSA_ERR_INVALID, "left and right must be -1 or more, sinks 0 or more");
-  if (!(s.scale >= 0.f) || std::isinf(s.scale)) return fail(BSA_ERR_INVALID, "scale must be positive and finite (or 0)");
+  if (!(s.scale >= 0.f) || std::isinf(s.scale * kLog2e)) return fail(BSA_ERR_INVALID, "scale must be positive and finite (or 0)");
   if (s.reserved != 0) return fail(BSA_ERR_INVALID, "reserved must be 0");
   if (s.dtype != BSA_DTYPE_BF16 && s.dtype != BSA_DTYPE_F16)
     return fail(BSA_ERR_UNSUPPORTED, "only bfloat16 and float16 tensors are implemented");
@@ -115,7 +116,7 @@ WindowArgs window_args(const bsa_window_shapes& s) {
   a.right = s.right < 0 || s.right > kFar ? kFar : s.right;
   a.sinks = std::min(s.sinks, s.seq_kv);
   a.scale = s.scale > 0.f ? s.scale : 1.f / std::sqrt((float)s.head_dim);
-  a.scale_log2 = a.scale * 1.44269504088896340736f;
+  a.scale_log2 = a.scale * kLog2e;
   return a;
 }
 
@@ -135,7 +136,7 @@ bsa_status check_workspace(int64_t need, const void* workspace, size_t bytes) {
 // A result is not written over a tensor that other workgroups still read.
 bsa_status check_apart(const char* name, const void* out, std::initializer_list<const void*> inputs) {
   for (const void* p : inputs)
-    if (out && out == p) return fail(BSA_ERR_INVALID, "%s is one of the inputs", name);
+    if (out && out == p) return fail(BSA_ERR_INVALID, "%s is one of the inputs or of the other outputs", name);
   return BSA_OK;
 }
 
@@ -200,6 +201,8 @@ bsa_status bsa_rope(const bsa_rope_shapes* shapes, const double* freq, const int
     TRY(check_tensor({"v", v, s.v_stride, s.batch, s.kv_heads, s.seq, s.head_dim, false}, size));
     TRY(check_tensor({"v_out", v_out, s.v_out_stride, s.batch, s.kv_heads, kv_rows, s.head_dim, true}, size));
   }
+  const void *kin = with_k ? k : nullptr, *vin = with_v ? v : nullptr;
+  void *kout = with_k ? k_out : nullptr, *vout = with_v ? v_out : nullptr;
   if (rows && ((with_k && k_out == k) || (with_v && v_out == v)))
     return fail(BSA_ERR_INVALID, "k and v cannot be turned in place when rows moves them");
 
@@ -209,16 +212,20 @@ bsa_status bsa_rope(const bsa_rope_shapes* shapes, const double* freq, const int
     const int64_t *xs, *ys;
     int64_t heads;
   } pair[3] = {{"q", q, q_out, s.q_stride, s.q_out_stride, s.heads},
-               {"k", with_k ? k : nullptr, k_out, s.k_stride, s.k_out_stride, s.kv_heads},
-               {"v", with_v ? v : nullptr, v_out, s.v_stride, s.v_out_stride, s.kv_heads}};
+               {"k", kin, k_out, s.k_stride, s.k_out_stride, s.kv_heads},
+               {"v", vin, v_out, s.v_stride, s.v_out_stride, s.kv_heads}};
   for (const auto& p : pair) {
     if (p.x && p.x == p.y && ((s.batch > 1 && p.xs[0] != p.ys[0]) || (p.heads > 1 && p.xs[1] != p.ys[1]) ||
                               (s.seq > 1 && p.xs[2] != p.ys[2])))
       return fail(BSA_ERR_INVALID, "%s is turned in place with other strides", p.name);
   }
 
-  const void* x[3] = {q, with_k ? k : nullptr, with_v ? v : nullptr};
-  void* y[3] = {q_out, k_out, v_out};
+  TRY(check_apart("q_out", q_out, {kin, vin, kout, vout}));
+  TRY(check_apart("k_out", kout, {q, vin, vout}));
+  TRY(check_apart("v_out", vout, {q, kin}));
+
+  const void* x[3] = {q, kin, vin};
+  void* y[3] = {q_out, kout, vout};
   const int64_t* xs[3] = {s.q_stride, s.k_stride, s.v_stride};
   const int64_t* ys[3] = {s.q_out_stride, s.k_out_stride, s.v_out_stride};
   for (int t = 0; t < 3; ++t) {

@@ -174,7 +174,7 @@ hipError_t launch(const RopeArgs& a, hipStream_t s) {
   if (lanes > 4 && tokens * items * 4 >= kFill) lanes = 4;
   const int per_block = kThreads / (items * lanes);
   const int64_t blocks = (tokens + per_block - 1) / per_block;
-  if (blocks > 0x7fffffff) return hipErrorInvalidValue;
+  if (!fits_launch(blocks, kThreads)) return hipErrorInvalidConfiguration;
   hipLaunchKernelGGL((rope_kernel<T, M>), dim3((unsigned)blocks), dim3(kThreads), 0, s, a, items, lanes, per_block);
   return hipGetLastError();
 }

@@ -432,7 +432,7 @@ __global__ __launch_bounds__(256) void window_dkv_sum_kernel(WindowArgs a) {
 template <typename T, int D>
 hipError_t launch(const WindowArgs& a, hipStream_t s) {
   const int64_t bh = (int64_t)a.B * a.Hkv, nq = a.ntiles * bh, nk = dkv_items(a) * bh;
-  if (nq > 0x7fffffff || nk > 0x7fffffff) return hipErrorInvalidValue;
+  if (!fits_launch(nq, 64 * kWaves) || !fits_launch(nk, 64 * kWaves)) return hipErrorInvalidConfiguration;
   if (nq > 0) {
     hipLaunchKernelGGL((window_dq_kernel<T, D>), dim3((unsigned)nq), dim3(64 * kWaves), 0, s, a);
     const hipError_t e = hipGetLastError();

@@ -658,7 +658,8 @@ template <typename T, int D>
 hipError_t launch(const WindowArgs& a, const ForwardPlan& p, hipStream_t s) {
   const int64_t n = (int64_t)p.ntiles * p.nsplit * a.B * a.Hkv;
   if (n == 0) return hipSuccess;
-  if (n > 0x7fffffff) return hipErrorInvalidValue;
+  const int64_t rows = (int64_t)a.B * a.Hkv * a.Nq * a.group;
+  if (!fits_launch(n, p.tile_rows * 2) || (p.nsplit > 1 && !fits_launch(rows, 256))) return hipErrorInvalidConfiguration;
   if (p.tile_rows == 32)
     hipLaunchKernelGGL((window_fwd_kernel<T, D, 1>), dim3((unsigned)n), dim3(64), 0, s, a);
   else if constexpr (D == 128)
@@ -667,7 +668,6 @@ hipError_t launch(const WindowArgs& a, const ForwardPlan& p, hipStream_t s) {
     hipLaunchKernelGGL((window_fwd_kernel<T, D, 4>), dim3((unsigned)n), dim3(256), 0, s, a);
   hipError_t e = hipGetLastError();
   if (e != hipSuccess || p.nsplit == 1) return e;
-  const int64_t rows = (int64_t)a.B * a.Hkv * a.Nq * a.group;
   if (p.nsplit <= 8) hipLaunchKernelGGL((window_join_kernel<T, D, 1>), dim3((unsigned)((rows + 3) / 4)), dim3(256), 0, s, a);
   else hipLaunchKernelGGL((window_join_kernel<T, D, 4>), dim3((unsigned)rows), dim3(256), 0, s, a);
   return hipGetLastError();

@@ -18,7 +18,6 @@ from __future__ import annotations
 import contextlib
 import ctypes
 import functools
-import math
 import struct
 from typing import Optional, Sequence, Tuple
 
@@ -227,8 +226,8 @@ def _window_head(q, k, v, left, right, sinks, scale):
     vs = _rows("v", v, dev, dtype, k_shape)
     if scale is None:
         scale = 0.0
-    elif not (scale > 0 and math.isfinite(scale)):
-        raise ValueError("scale must be positive and finite")
+    elif not (1e-37 < scale < 1e38):  # (0 in 32 bits asks for the default)
+        raise ValueError("scale must be positive and finite in 32 bits")
     fields = (B, H, Hkv, Nq, Nkv, d, code, min(left, _INT_MAX), min(right, _INT_MAX), min(sinks, _INT_MAX), scale, 0,
               qs[0], qs[2], qs[1], ks[0], ks[2], ks[1], vs[0], vs[2], vs[1])
     return dev, dtype, q_shape, k_shape, fields

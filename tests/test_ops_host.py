@@ -249,6 +249,32 @@ def test_rope_refusals(kw, status, word):
     assert word in LIB.bsa_ops_last_error().decode()
 
 
+@pytest.mark.parametrize("same", [("q_out", "k"), ("q_out", "v"), ("q_out", "k_out"), ("q_out", "v_out"), ("k_out", "q"),
+                                  ("k_out", "v"), ("k_out", "v_out"), ("v_out", "q"), ("v_out", "k")])
+def test_rope_outputs_stay_apart(same):
+    p = {x: PTR * (1 + i) for i, x in enumerate(("q", "k", "v", "q_out", "k_out", "v_out"))}
+    p[same[0]] = p[same[1]]
+    assert rope(ptrs=p) == INVALID and same[0] in LIB.bsa_ops_last_error().decode()
+
+
+def test_scale_that_leaves_32_bits():
+    assert forward(window(scale=3e38)) == INVALID and "scale" in LIB.bsa_ops_last_error().decode()
+
+
+def test_launches_of_too_many_threads():
+    """2^32 threads and more are an error of the call, before anything runs."""
+    one = dict(batch=1 << 27, heads=1, kv_heads=1, seq_q=1, seq_kv=1)
+    assert forward(window(**one)) == _ffi.BSA_ERR_HIP and "configuration" in LIB.bsa_ops_last_error().decode()
+    s = window(**one)
+    assert backward(s, grads(s)) == _ffi.BSA_ERR_HIP and "configuration" in LIB.bsa_ops_last_error().decode()
+    n = 1 << 10
+    st = (n * 256, 64, 256)
+    kv = (n * 128, 64, 128)
+    assert rope(batch=1 << 20, seq=n, kv_rows=n, q_stride=st, q_out_stride=st, k_stride=kv, v_stride=kv, k_out_stride=kv,
+                v_out_stride=kv, ptrs=dict(k_out=3 * PTR, v_out=4 * PTR)) == _ffi.BSA_ERR_HIP
+    assert "configuration" in LIB.bsa_ops_last_error().decode()
+
+
 def test_binding_refusals_on_the_host():
     import torch
     t = torch.zeros((1, 4, 2, 64), dtype=torch.bfloat16)
