@@ -218,12 +218,15 @@ __global__ __launch_bounds__(64 * kWaves) __attribute__((amdgpu_waves_per_eu(2, 
   __shared__ __attribute__((aligned(1024))) uint8_t ring1[kSlot];
   auto slot = [&](int i) -> uint8_t* { return i == 0 ? ring0 : ring1; };
 
-  const int64_t items = dkv_items(a), item = item_of_slot(blockIdx.x, items * a.B * a.Hkv);
-  const int bh = (int)(item / items), in_head = (int)(item % items);
-  const int plain = (a.nktiles - a.nsink) * a.slices;  // items of the tiles without sinks
-  const bool sink = in_head >= plain;
-  const int nslice = sink ? a.sink_slices : a.slices;
-  const int in_kind = sink ? in_head - plain : in_head;
+  // The tiles without sinks of every head come first, then the others: each kind is
+  // spread over the XCDs by itself (in one list, where some XCDs get most of the sinks'
+  // slices: 270 us for 239 at 8192 queries, 16 heads over 4, window 1024, 4 sinks).
+  const int heads = a.B * a.Hkv, plain = (a.nktiles - a.nsink) * a.slices;
+  const int64_t all_plain = (int64_t)plain * heads;
+  const bool sink = blockIdx.x >= all_plain;
+  const int of_kind = sink ? a.nsink * a.sink_slices : plain, nslice = sink ? a.sink_slices : a.slices;
+  const int64_t item = item_of_slot(blockIdx.x - (sink ? all_plain : 0), (int64_t)of_kind * heads);
+  const int bh = (int)(item / of_kind), in_kind = (int)(item % of_kind);
   const int tile = in_kind / nslice + (sink ? 0 : a.nsink), slice = in_kind % nslice;
   const int b = bh / a.Hkv, kvh = bh % a.Hkv;
   const Seq sq(a, b);
