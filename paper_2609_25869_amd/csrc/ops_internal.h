@@ -68,6 +68,7 @@ struct WindowArgs {
   // dK/dV: key tiles per key head, those that hold sinks (the first ones), and the
   // slices that the queries of a tile with and without sinks are cut into
   int32_t nktiles, nsink, sink_slices, slices;
+  int32_t deep;  // which dK/dV kernel
 };
 
 // Key tiles of one key head as work items of the dK/dV kernel: the slices of the

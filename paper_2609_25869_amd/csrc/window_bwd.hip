@@ -17,6 +17,8 @@
 // lane, which is the layout that the products over the walked rows need.  Two
 // workgroups of four waves share a CU; walked rows come in tiles of 64 through two
 // ring slots (with 32 and four slots, twice the barriers: dK/dV 6.9 ms for 6.3).
+// Where there are too few workgroups for two on a CU, a second form of the dK/dV kernel
+// makes up for the missing wave within one.
 //
 // P, and dS after its subtraction, are rounded to the tensors' type for the products
 // (float16 holds dS below 2^-14 to 2^-25: scale the loss where gradients are that
@@ -203,20 +205,27 @@ struct Seen {
   }
 };
 
-template <typename T, int D>
-__global__ __launch_bounds__(64 * kWaves) __attribute__((amdgpu_waves_per_eu(2, 2))) void window_dkv_kernel(WindowArgs a) {
+// Deep: one wave per SIMD with all the registers, three ring slots, and the products of
+// a tile in one sequence that nothing interrupts: operands are read four products ahead,
+// and the probabilities of one half are formed between the products of the other.  A tile
+// of 64 rows takes a workgroup 2.3 us, where the plain kernel takes 3.3 alone on its CU
+// and 3.9 with another beside it.  (Operands six ahead: the same.)
+template <typename T, int D, bool Deep>
+__global__ __launch_bounds__(64 * kWaves) __attribute__((amdgpu_waves_per_eu(Deep ? 1 : 2, Deep ? 1 : 2)))
+void window_dkv_kernel(WindowArgs a) {
 #ifdef __HIP_DEVICE_COMPILE__
   using E = Elem<T>;
   using R = Rows<D>;
   typedef typename E::x8 x8;
-  constexpr int TR = 64, TKEY = 32 * kWaves, kStages = 2;
+  constexpr int TR = 64, TKEY = 32 * kWaves, kStages = Deep ? 3 : 2;
   constexpr int kTile = TR * R::kBytes, kStat = 512;
   using Load = TileLoad<D, TR, kWaves>;
   constexpr int kGroup = 2 * Load::kLoads + 2;
   constexpr int kSlot = 2 * kTile + kWaves * kStat;  // Q, dO, and LSE and D of the rows, a copy per wave
   __shared__ __attribute__((aligned(1024))) uint8_t ring0[kSlot];
   __shared__ __attribute__((aligned(1024))) uint8_t ring1[kSlot];
-  auto slot = [&](int i) -> uint8_t* { return i == 0 ? ring0 : ring1; };
+  __shared__ __attribute__((aligned(1024))) uint8_t ring2[Deep ? kSlot : 16];
+  auto slot = [&](int i) -> uint8_t* { return i == 0 ? ring0 : i == 1 ? ring1 : ring2; };
 
   // The tiles without sinks of every head come first, then the others: each kind is
   // spread over the XCDs by itself (in one list, where some XCDs get most of the sinks'
@@ -309,63 +318,146 @@ __global__ __launch_bounds__(64 * kWaves) __attribute__((amdgpu_waves_per_eu(2, 
       wait_vm_lgkm<(kStages - 2) * kGroup>();
       block_sync();
       issue(slot((u + kStages - 1) % kStages));
-      auto half = [&](auto blk) BSA_INLINE {
-        constexpr int rb = decltype(blk)::value;
-        const int i_blk = i_now + 32 * rb;
-        const uint8_t* qs = slot(u) + rb * 32 * R::kBytes;
-        const uint8_t* gs = qs + kTile;
+      if constexpr (Deep) {
         int ro = roff, t0 = toff0, t1 = toff1;
-        asm volatile("" : "+v"(ro), "+v"(t0), "+v"(t1));  // formed again per tile: sixteen addresses would not fit
-        const uint8_t* st = slot(u) + 2 * kTile + w * kStat + 128 * rb + 16 * (lane_now() >> 5);
-        f32x16 s = {}, dp = {};
+        asm volatile("" : "+v"(ro), "+v"(t0), "+v"(t1));  // formed again per tile
+        // Products in their order, kP of them a phase: scores (S, dP in turn) of half 0, of
+        // half 1, then dV and dK in turn of half 0, of half 1.
+        constexpr int kP = 2 * R::kSteps, kUnits = 4 * kP;
+        static_assert(kP == 16, "a phase forms one of a lane's 16 probabilities per product");
+        const uint8_t* qs = slot(u);
+        const uint8_t* gs = qs + kTile;
+        auto load_op = [&](int i) BSA_INLINE -> x8 {
+          const int ph = i / kP, j = i % kP, rows = (ph & 1) * 32 * R::kBytes;
+          if (ph < 2) return *reinterpret_cast<const x8*>((j % 2 ? gs : qs) + rows + (ro ^ ((j / 2) << 5)));
+          const int c = j / (2 * R::kBlocks), d = j / 2 % R::kBlocks, o = rows + c * 16 * R::kBytes;
+          const uint8_t* x = j % 2 ? qs : gs;
+          return read_tr_pair<T>(x + o + (t0 ^ (d << 6)), x + o + (t1 ^ (d << 6)));
+        };
+        const uint8_t* st = slot(u) + 2 * kTile + w * kStat + 16 * (lane_now() >> 5);
+        constexpr int kAhead = 4;
+        x8 op[kAhead + 1];
 #pragma unroll
-        for (int c = 0; c < R::kSteps; ++c) {
-          s = E::mfma(*reinterpret_cast<const x8*>(qs + (ro ^ (c << 5))), kf[c], s);
-          dp = E::mfma(*reinterpret_cast<const x8*>(gs + (ro ^ (c << 5))), vf[c], dp);
-        }
-        const bool full = i_blk >= full_lo && i_blk + 31 <= full_hi;
+        for (int i = 0; i < kAhead; ++i) op[i] = load_op(i);
+        f32x16 s[2] = {}, dp[2] = {};
+        u32x4 p[2][2], q[2][2];
         float pv[16], ds[16];
+        f32x4 lse[2], delta[2];
+        auto load_stat = [&](int h, int r4) BSA_INLINE {
+          lse[r4 & 1] = *reinterpret_cast<const f32x4*>(st + 128 * h + 32 * r4);
+          delta[r4 & 1] = *reinterpret_cast<const f32x4*>(st + 128 * h + 256 + 32 * r4);
+        };
+        auto form = [&](int h, int e) BSA_INLINE {
+          const int r4 = e / 4;
+          if (e % 4 == 0 && r4 < 3) load_stat(h, r4 + 1);
+          pv[e] = fast_exp2(__builtin_fmaf(s[h][e], a.scale_log2, -lse[r4 & 1][e % 4]));
+          ds[e] = dp[h][e] - delta[r4 & 1][e % 4];
+        };
+        auto pack = [&](int h, int e) BSA_INLINE {
+          p[h][e / 8][(e % 8) / 2] = pack2<T>(pv[e], pv[e + 1]);
+          q[h][e / 8][(e % 8) / 2] = pack2<T>(pv[e] * ds[e], pv[e + 1] * ds[e + 1]);
+        };
+        auto mask = [&](int h) BSA_INLINE {
+          const int i_blk = i_now + 32 * h;
+          if (__builtin_expect(i_blk >= full_lo && i_blk + 31 <= full_hi, 1)) return;
+          const int l = lane_now(), key = kw + (l & 31);
+          const uint32_t bits = (bits_below(seen.last(key) - i_blk + 1) & ~bits_below(seen.first(key) - i_blk)) >> (4 * (l >> 5));
 #pragma unroll
-        for (int r4 = 0; r4 < 4; ++r4) {
-          const f32x4 lse = *reinterpret_cast<const f32x4*>(st + 32 * r4);
-          const f32x4 delta = *reinterpret_cast<const f32x4*>(st + 256 + 32 * r4);
-#pragma unroll
-          for (int e = 0; e < 4; ++e) {
-            const int i = 4 * r4 + e;
-            pv[i] = fast_exp2(__builtin_fmaf(s[i], a.scale_log2, -lse[e]));
-            ds[i] = pv[i] * (dp[i] - delta[e]);
+          for (int i = 0; i < 16; i += 2) {
+            const uint32_t b2 = bits >> (8 * (i >> 2) + (i & 3));
+            const uint32_t keep = (b2 & 1u ? 0xffffu : 0u) | (b2 & 2u ? 0xffff0000u : 0u);
+            uint32_t x = p[h][i / 8][(i % 8) / 2], y = q[h][i / 8][(i % 8) / 2];
+            asm volatile("v_and_b32 %0, %2, %0\n\tv_and_b32 %1, %2, %1" : "+v"(x), "+v"(y) : "v"(keep));
+            p[h][i / 8][(i % 8) / 2] = x;
+            q[h][i / 8][(i % 8) / 2] = y;
+          }
+        };
+        each_slot<kUnits>([&](auto unit) BSA_INLINE -> bool {
+          constexpr int i = decltype(unit)::value, ph = i / kP, j = i % kP;
+          if (i + kAhead < kUnits) op[(i + kAhead) % (kAhead + 1)] = load_op(i + kAhead);
+          const x8 x = op[i % (kAhead + 1)];
+          if (j == kP - 1 && ph < 2) load_stat(ph, 0);
+          if (ph < 2) {
+            if (j % 2 == 0) s[ph] = E::mfma(x, kf[j / 2], s[ph]);
+            else dp[ph] = E::mfma(x, vf[j / 2], dp[ph]);
+          } else {
+            const int c = j / (2 * R::kBlocks), d = j / 2 % R::kBlocks, h = ph - 2;
+            if (j % 2 == 0) dv[d] = E::mfma(x, __builtin_bit_cast(x8, p[h][c]), dv[d]);
+            else dk[d] = E::mfma(x, __builtin_bit_cast(x8, q[h][c]), dk[d]);
+          }
+          // half 0's probabilities beside the scores of half 1, half 1's beside the
+          // products of half 0
+          if (ph == 1 || ph == 2) {
+            const int h = ph - 1;
+            if (j > 0 && j % 2 == 0) pack(h, j - 2);
+            form(h, j);
+            if (j == kP - 1) {
+              pack(h, 14);
+              mask(h);
+            }
           }
           __builtin_amdgcn_sched_barrier(0);
-        }
-        if (__builtin_expect(!full, 0)) {
-          const int l = lane_now(), key = kw + (l & 31);
-          const uint32_t bits =
-              (bits_below(seen.last(key) - i_blk + 1) & ~bits_below(seen.first(key) - i_blk)) >> (4 * (l >> 5));
+          return true;
+        });
+      } else {
+        auto half = [&](auto blk) BSA_INLINE {
+          constexpr int rb = decltype(blk)::value;
+          const int i_blk = i_now + 32 * rb;
+          const uint8_t* qs = slot(u) + rb * 32 * R::kBytes;
+          const uint8_t* gs = qs + kTile;
+          int ro = roff, t0 = toff0, t1 = toff1;
+          asm volatile("" : "+v"(ro), "+v"(t0), "+v"(t1));  // formed again per tile: sixteen addresses would not fit
+          const uint8_t* st = slot(u) + 2 * kTile + w * kStat + 128 * rb + 16 * (lane_now() >> 5);
+          f32x16 s = {}, dp = {};
 #pragma unroll
-          for (int i = 0; i < 16; ++i) {
-            const bool see = (bits >> (8 * (i >> 2) + (i & 3))) & 1u;
-            zero_unless(pv[i], see);
-            zero_unless(ds[i], see);
+          for (int c = 0; c < R::kSteps; ++c) {
+            s = E::mfma(*reinterpret_cast<const x8*>(qs + (ro ^ (c << 5))), kf[c], s);
+            dp = E::mfma(*reinterpret_cast<const x8*>(gs + (ro ^ (c << 5))), vf[c], dp);
           }
-        }
-        u32x4 p[2], q[2];
+          const bool full = i_blk >= full_lo && i_blk + 31 <= full_hi;
+          float pv[16], ds[16];
 #pragma unroll
-        for (int i = 0; i < 16; i += 2) {
-          p[i / 8][(i % 8) / 2] = pack2<T>(pv[i], pv[i + 1]);
-          q[i / 8][(i % 8) / 2] = pack2<T>(ds[i], ds[i + 1]);
-        }
+          for (int r4 = 0; r4 < 4; ++r4) {
+            const f32x4 lse = *reinterpret_cast<const f32x4*>(st + 32 * r4);
+            const f32x4 delta = *reinterpret_cast<const f32x4*>(st + 256 + 32 * r4);
 #pragma unroll
-        for (int c = 0; c < 2; ++c) {
-#pragma unroll
-          for (int d = 0; d < R::kBlocks; ++d) {
-            const int o0 = c * 16 * R::kBytes + (t0 ^ (d << 6)), o1 = c * 16 * R::kBytes + (t1 ^ (d << 6));
-            dv[d] = E::mfma(read_tr_pair<T>(gs + o0, gs + o1), __builtin_bit_cast(x8, p[c]), dv[d]);
-            dk[d] = E::mfma(read_tr_pair<T>(qs + o0, qs + o1), __builtin_bit_cast(x8, q[c]), dk[d]);
+            for (int e = 0; e < 4; ++e) {
+              const int i = 4 * r4 + e;
+              pv[i] = fast_exp2(__builtin_fmaf(s[i], a.scale_log2, -lse[e]));
+              ds[i] = pv[i] * (dp[i] - delta[e]);
+            }
+            __builtin_amdgcn_sched_barrier(0);
           }
-        }
-      };
-      half(std::integral_constant<int, 0>{});
-      half(std::integral_constant<int, 1>{});
+          if (__builtin_expect(!full, 0)) {
+            const int l = lane_now(), key = kw + (l & 31);
+            const uint32_t bits =
+                (bits_below(seen.last(key) - i_blk + 1) & ~bits_below(seen.first(key) - i_blk)) >> (4 * (l >> 5));
+#pragma unroll
+            for (int i = 0; i < 16; ++i) {
+              const bool see = (bits >> (8 * (i >> 2) + (i & 3))) & 1u;
+              zero_unless(pv[i], see);
+              zero_unless(ds[i], see);
+            }
+          }
+          u32x4 p[2], q[2];
+#pragma unroll
+          for (int i = 0; i < 16; i += 2) {
+            p[i / 8][(i % 8) / 2] = pack2<T>(pv[i], pv[i + 1]);
+            q[i / 8][(i % 8) / 2] = pack2<T>(ds[i], ds[i + 1]);
+          }
+#pragma unroll
+          for (int c = 0; c < 2; ++c) {
+#pragma unroll
+            for (int d = 0; d < R::kBlocks; ++d) {
+              const int o0 = c * 16 * R::kBytes + (t0 ^ (d << 6)), o1 = c * 16 * R::kBytes + (t1 ^ (d << 6));
+              dv[d] = E::mfma(read_tr_pair<T>(gs + o0, gs + o1), __builtin_bit_cast(x8, p[c]), dv[d]);
+              dk[d] = E::mfma(read_tr_pair<T>(qs + o0, qs + o1), __builtin_bit_cast(x8, q[c]), dk[d]);
+            }
+          }
+        };
+        half(std::integral_constant<int, 0>{});
+        half(std::integral_constant<int, 1>{});
+      }
       i_now += TR;
       if (i_now > i_hi) i_now = i_lo;
       return true;
@@ -442,7 +534,8 @@ hipError_t launch(const WindowArgs& a, hipStream_t s) {
     if (e != hipSuccess) return e;
   }
   if (nk == 0) return hipSuccess;
-  hipLaunchKernelGGL((window_dkv_kernel<T, D>), dim3((unsigned)nk), dim3(64 * kWaves), 0, s, a);
+  if (D == 128 && a.deep) hipLaunchKernelGGL((window_dkv_kernel<T, 128, true>), dim3((unsigned)nk), dim3(64 * kWaves), 0, s, a);
+  else hipLaunchKernelGGL((window_dkv_kernel<T, D, false>), dim3((unsigned)nk), dim3(64 * kWaves), 0, s, a);
   hipError_t e = hipGetLastError();
   const int64_t cut = (a.sink_slices > 1 ? a.nsink : 0) + (a.slices > 1 ? a.nktiles - a.nsink : 0);
   if (e != hipSuccess || cut == 0) return e;
@@ -465,19 +558,31 @@ int64_t plan_backward(WindowArgs* a, int d) {
   const int64_t walk_sink = ((int64_t)a->Nq + 63) / 64 * a->group;
   const int64_t walk = min64(walk_sink, ((int64_t)a->left + a->right + kKeys + 63) / 64 * a->group);
   a->nsink = (int32_t)((a->sinks + kKeys - 1) / kKeys);
-  // Slices.  A slice costs 128 KB (head dim 128) written and read again, and two
-  // workgroups share a CU: tiles without sinks are cut only where they are fewer than
-  // three quarters of the CUs (twice that where walks span much of the sequence, and so
-  // are of very different lengths; one key head, 4096 tokens, all keys before: 300 us with
-  // 256 workgroups, 238 with 512).  Tiles with sinks are cut to the others' walk, and to a
-  // quarter of it where there are few workgroups, so that they fill the gaps behind the
-  // longer ones (they come last).  No slice is shorter than four row tiles, and the slices
-  // of sinks take half a gigabyte at most.
+  // Which dK/dV kernel.  Two workgroups of the plain one share a CU, one of the deep one
+  // has a CU to itself: deep where no CU would get two (8192 queries, window 1024, 3
+  // heads: 97 us for dQ, dK and dV with the plain kernel, 79 with the deep one; 6 heads:
+  // 133 and 141), and up to twice that where walks span much of the sequence and so are
+  // of very different lengths (all keys before, 6 heads: 603 and 500; 12: 854 and 875).
+  //
+  // Slices.  A slice costs 128 KB (head dim 128) written and read again.  Tiles without
+  // sinks are cut only where they are few: less than three quarters of the CUs, or half
+  // for the deep kernel (twice that where walks are uneven; one key head, 4096 tokens,
+  // all keys before: 300 us with 256 workgroups, 238 with 512).  Tiles with sinks come
+  // last, to fill the gaps behind the longer ones: they are cut to the others' walk, to a
+  // quarter of it where there are few workgroups, and for the deep kernel to one more
+  // workgroup for every CU.  No slice is shorter than four row tiles, and the slices of
+  // sinks take half a gigabyte at most.
   const int64_t bh = max64((int64_t)a->B * a->Hkv, 1), plain = bh * (a->nktiles - a->nsink);
   const int64_t want = 2 * walk > walk_sink ? 512 : 256;
-  const int64_t cut = plain > 0 && 4 * plain < 3 * want ? (want + plain - 1) / plain : 1;
+  a->deep = d == 128 && bh * a->nktiles <= want;
+  const int64_t cut = plain <= 0             ? 1
+                      : a->deep              ? want / plain
+                      : 4 * plain < 3 * want ? (want + plain - 1) / plain
+                                             : 1;
   const int64_t goal = max64((walk + cut - 1) / cut, 4);
-  const int64_t goal_sink = bh * a->nktiles < 1024 ? max64((goal + 3) / 4, 4) : goal;
+  const int64_t goal_sink = a->deep                  ? max64((walk_sink * a->nsink * bh + 255) / 256, 4)
+                            : bh * a->nktiles < 1024 ? max64((goal + 3) / 4, 4)
+                                                     : goal;
   const int64_t most_sink = max64(4096 / (bh * max64(a->nsink, 1)), 1);
   a->slices = (int32_t)max64(1, min64((walk + goal - 1) / goal, 256));
   a->sink_slices = (int32_t)max64(1, min64((walk_sink + goal_sink - 1) / goal_sink, min64(most_sink, 256)));
