@@ -210,8 +210,10 @@ struct Seen {
 // and the probabilities of one half are formed between the products of the other.  A tile
 // of 64 rows takes a workgroup 2.3 us, where the plain kernel takes 3.3 alone on its CU
 // and 3.9 with another beside it.  (Operands six ahead: the same.)
+// Three workgroups share a CU at head dim 64 (16384 tokens, 16 heads, window 1024: 386 us
+// for dQ, dK and dV with two, 357 with three).
 template <typename T, int D, bool Deep>
-__global__ __launch_bounds__(64 * kWaves) __attribute__((amdgpu_waves_per_eu(Deep ? 1 : 2, Deep ? 1 : 2)))
+__global__ __launch_bounds__(64 * kWaves) __attribute__((amdgpu_waves_per_eu(Deep ? 1 : D == 64 ? 3 : 2, Deep ? 1 : D == 64 ? 3 : 2)))
 void window_dkv_kernel(WindowArgs a) {
 #ifdef __HIP_DEVICE_COMPILE__
   using E = Elem<T>;
