@@ -7,7 +7,7 @@
 //         Sinks are seen by every later query: a tile with sinks is cut into
 //         slices of its queries, of about the length of the other tiles' walks,
 //         and a third kernel adds the slices' sums up in order.  (8192 queries, 16
-//         heads over 4 key heads, window 1024, 4 sinks: 1626 us in one piece.)
+//         heads over 4 key heads, window 1024, 4 sinks: 1626 us in one piece, 190 so.)
 //
 //   P = exp(S - LSE), dS = P o (dO V^T - D)
 //   dQ = scale dS K, dV = P^T dO, dK = scale dS^T Q
@@ -53,9 +53,9 @@ __global__ __launch_bounds__(64 * kWaves) void window_dq_kernel(WindowArgs a) {
   __shared__ __attribute__((aligned(1024))) uint8_t ring1[2 * kTile];
   auto slot = [&](int i) -> uint8_t* { return i == 0 ? ring0 : ring1; };
 
-  const int64_t item = item_of_slot(blockIdx.x, (int64_t)a.ntiles * a.B * a.Hkv);
-  const int tile = (int)(item % a.ntiles), bh = (int)(item / a.ntiles);
-  const int b = bh / a.Hkv, kvh = bh % a.Hkv;
+  int b;
+  const uint32_t item = item_of_slot(blockIdx.x, (uint32_t)a.ntiles * a.Hkv, &b);
+  const int tile = (int)(item % a.ntiles), kvh = (int)(item / a.ntiles);
   const Seq sq(a, b);
   const int nrows = sq.q_len * a.group, r0 = tile * TQ;
   if (r0 >= nrows) return;
@@ -232,14 +232,14 @@ void window_dkv_kernel(WindowArgs a) {
   // The tiles without sinks of every head come first, then the others: each kind is
   // spread over the XCDs by itself (in one list, where some XCDs get most of the sinks'
   // slices: 270 us for 239 at 8192 queries, 16 heads over 4, window 1024, 4 sinks).
-  const int heads = a.B * a.Hkv, plain = (a.nktiles - a.nsink) * a.slices;
-  const int64_t all_plain = (int64_t)plain * heads;
+  const int plain = (a.nktiles - a.nsink) * a.slices;  // items per key head
+  const uint32_t all_plain = (uint32_t)plain * a.Hkv * a.B;
   const bool sink = blockIdx.x >= all_plain;
   const int of_kind = sink ? a.nsink * a.sink_slices : plain, nslice = sink ? a.sink_slices : a.slices;
-  const int64_t item = item_of_slot(blockIdx.x - (sink ? all_plain : 0), (int64_t)of_kind * heads);
-  const int bh = (int)(item / of_kind), in_kind = (int)(item % of_kind);
+  int b;
+  const uint32_t item = item_of_slot(blockIdx.x - (sink ? all_plain : 0), (uint32_t)of_kind * a.Hkv, &b);
+  const int kvh = (int)(item / of_kind), in_kind = (int)(item % of_kind), bh = b * a.Hkv + kvh;
   const int tile = in_kind / nslice + (sink ? 0 : a.nsink), slice = in_kind % nslice;
-  const int b = bh / a.Hkv, kvh = bh % a.Hkv;
   const Seq sq(a, b);
   const int k0 = tile * TKEY;
   if (k0 >= sq.kv_len) return;

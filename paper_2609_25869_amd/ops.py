@@ -10,8 +10,8 @@ their own (rope with inverse=True, window_backward).
 A call of a few microseconds on the device is bound by what the host does for
 it, so the checks take each tensor's properties once, the shape structures are
 packed in one go, and the device is only changed where it differs.  (One token
-of one stream over a cache, two launches: 21 us with a structure filled field by
-field and a device context around every call.)
+of one stream over a cache, two launches of 10 us: 14 us a call, and 21 with a
+structure filled field by field and a device context around every call.)
 """
 from __future__ import annotations
 
