@@ -54,6 +54,8 @@ struct WindowArgs {
   float scale_log2;            // scale * log2(e)
   const int32_t* q_len;
   const int32_t* kv_len;
+  int32_t deal;          // see item_of_slot
+  int32_t later_longer;  // rows see the more keys the later they are
   int32_t ntiles;  // row tiles per key head
   int32_t nsplit;  // slices of a row tile's keys (forward)
   float* part;     // partial states of the slices

@@ -54,8 +54,8 @@ __global__ __launch_bounds__(64 * kWaves) void window_dq_kernel(WindowArgs a) {
   auto slot = [&](int i) -> uint8_t* { return i == 0 ? ring0 : ring1; };
 
   int b;
-  const uint32_t item = item_of_slot(blockIdx.x, (uint32_t)a.ntiles * a.Hkv, &b);
-  const int tile = (int)(item % a.ntiles), kvh = (int)(item / a.ntiles);
+  const uint32_t item = item_of_slot(a, blockIdx.x, (uint32_t)a.ntiles, &b);
+  const int tile = tile_of(a, (int)(item % a.ntiles)), kvh = (int)(item / a.ntiles);
   const Seq sq(a, b);
   const int nrows = sq.q_len * a.group, r0 = tile * TQ;
   if (r0 >= nrows) return;
@@ -237,7 +237,7 @@ void window_dkv_kernel(WindowArgs a) {
   const bool sink = blockIdx.x >= all_plain;
   const int of_kind = sink ? a.nsink * a.sink_slices : plain, nslice = sink ? a.sink_slices : a.slices;
   int b;
-  const uint32_t item = item_of_slot(blockIdx.x - (sink ? all_plain : 0), (uint32_t)of_kind * a.Hkv, &b);
+  const uint32_t item = item_of_slot(a, blockIdx.x - (sink ? all_plain : 0), (uint32_t)of_kind, &b);
   const int kvh = (int)(item / of_kind), in_kind = (int)(item % of_kind), bh = b * a.Hkv + kvh;
   const int tile = in_kind / nslice + (sink ? 0 : a.nsink), slice = in_kind % nslice;
   const Seq sq(a, b);

@@ -244,18 +244,32 @@ __device__ inline void zero_unless(float& x, bool keep) {
   asm volatile("s_nop 1\n\tv_cndmask_b32_e64 %0, 0, %0, %1" : "+v"(x) : "s"(__ballot(keep)));
 }
 
-// Dispatch order: the eight XCDs take consecutive workgroups in turn, so slot s of n
-// runs work item (s % 8) * ceil(n / 8) + s / 8, which gives every XCD a contiguous share
-// of the items, in order: neighbouring row tiles of a head read nearly the same keys
-// through one L2.  Every sequence is spread over the XCDs by itself: with one list for the
-// batch, XCDs that get the short ones run dry (three sequences of up to 5001 tokens, 16
-// heads of 64, window 701: 73 us with one list, 63 so).
-__device__ inline uint32_t item_of_slot(uint32_t slot, uint32_t per_sequence, int* b) {
-  const uint32_t n = per_sequence, s = slot % n;
+// Dispatch order: the work item (of per_head in every key head, the heads of a sequence
+// one after the other) and the sequence that a slot runs.  The eight XCDs take consecutive
+// workgroups in turn.
+//
+// Every XCD gets a contiguous share of a sequence's items, in order: neighbouring row
+// tiles of a head read nearly the same keys through one L2.  Every sequence is shared out
+// by itself (with one list for the batch, XCDs that get the short ones run dry: three
+// sequences of up to 5001 tokens, 16 heads of 64, window 701: 73 us with one list, 63 so),
+// and the shares move on by one XCD from sequence to sequence.
+//
+// `deal`: the tiles are dealt out one by one instead, the first tile of every head and
+// sequence before the second, and the row of eight turned by one each time.
+__device__ inline uint32_t item_of_slot(const WindowArgs& a, uint32_t slot, uint32_t per_head, int* b) {
+  const uint32_t n = per_head * a.Hkv;
+  if (a.deal) {
+    const uint32_t k = slot / 8, i = 8 * k + 8 <= n * a.B ? 8 * k + (slot + k) % 8 : slot;
+    *b = (int)(i % a.B);
+    return i / a.B % a.Hkv * per_head + i / a.B / a.Hkv;
+  }
   *b = (int)(slot / n);
-  const uint32_t share = n / 8, more = n % 8, x = s % 8;
+  const uint32_t s = slot % n, share = n / 8, more = n % 8, x = more ? s % 8 : (s + *b) % 8;
   return x * share + (x < more ? x : more) + s / 8;
 }
+
+// The i-th row tile of a head: where later rows see more keys, the last one first.
+__device__ inline int tile_of(const WindowArgs& a, int i) { return a.later_longer ? a.ntiles - 1 - i : i; }
 
 }  // namespace
 }  // namespace bsa_ops

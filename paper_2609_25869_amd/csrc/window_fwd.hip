@@ -171,9 +171,9 @@ __global__ __launch_bounds__(64 * NW, NW == 4 ? 4 : 1) void window_fwd_kernel(Wi
   auto slot = [&](int i) -> uint8_t* { return i == 0 ? ring0 : ring1; };
 
   int b;
-  const uint32_t item = item_of_slot(blockIdx.x, (uint32_t)a.ntiles * a.nsplit * a.Hkv, &b);
+  const uint32_t item = item_of_slot(a, blockIdx.x, (uint32_t)a.ntiles * a.nsplit, &b);
   const int split = (int)(item % a.nsplit), rest = (int)(item / a.nsplit);
-  const int tile = rest % a.ntiles, kvh = rest / a.ntiles, bh = b * a.Hkv + kvh;
+  const int tile = tile_of(a, rest % a.ntiles), kvh = rest / a.ntiles, bh = b * a.Hkv + kvh;
   const Seq sq(a, b);
   const int nrows = sq.q_len * a.group, r0 = tile * TQ;
   if (r0 >= nrows) return;
@@ -355,9 +355,9 @@ void window_fwd_piped_kernel(WindowArgs a) {
   auto vslot = [&](int i) BSA_INLINE -> uint8_t* { return kslot(i) + kTile; };
 
   int b;
-  const uint32_t item = item_of_slot(blockIdx.x, (uint32_t)a.ntiles * a.nsplit * a.Hkv, &b);
+  const uint32_t item = item_of_slot(a, blockIdx.x, (uint32_t)a.ntiles * a.nsplit, &b);
   const int split = (int)(item % a.nsplit), rest = (int)(item / a.nsplit);
-  const int tile = rest % a.ntiles, kvh = rest / a.ntiles, bh = b * a.Hkv + kvh;
+  const int tile = tile_of(a, rest % a.ntiles), kvh = rest / a.ntiles, bh = b * a.Hkv + kvh;
   const Seq sq(a, b);
   const int nrows = sq.q_len * a.group, r0 = tile * TQ;
   if (r0 >= nrows) return;
