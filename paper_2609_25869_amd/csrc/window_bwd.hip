@@ -571,16 +571,16 @@ int64_t plan_backward(WindowArgs* a, int d) {
   a->nsink = (int32_t)((a->sinks + kKeys - 1) / kKeys);
   // Which dK/dV kernel.  Two workgroups of the plain one share a CU, one of the deep one
   // has a CU to itself: deep where no CU would get two (8192 queries, window 1024, 3
-  // heads: 97 us for dQ, dK and dV with the plain kernel, 79 with the deep one; 6 heads:
-  // 133 and 141), and up to twice that where walks span much of the sequence and so are
-  // of very different lengths (all keys before, 6 heads: 603 and 500; 12: 854 and 875).
+  // heads: 91 us for dQ, dK and dV with the plain kernel, 77 with the deep one; 6 heads:
+  // 128 and 139), and up to twice that where walks span much of the sequence and so are
+  // of very different lengths (all keys before, 8 heads: 566 and 479; 12: 700 and 714).
   //
   // Slices.  A slice costs 128 KB (head dim 128) written and read again.  Tiles without
   // sinks are cut only where they are few: less than three quarters of the CUs, or half
-  // for the deep kernel (twice that where walks are uneven; one key head, 4096 tokens,
-  // all keys before: 300 us with 256 workgroups, 238 with 512).  Tiles with sinks come
-  // last, to fill the gaps behind the longer ones: they are cut to the others' walk, to a
-  // quarter of it where there are few workgroups, and for the deep kernel to one more
+  // for the deep kernel (twice that where walks are uneven; one key head, 4096 tokens, all
+  // keys before, in shares: 300 us with 256 workgroups, 238 with 512).  Tiles with sinks
+  // come last, to fill the gaps behind the longer ones: they are cut to the others' walk,
+  // to a quarter of it where there are few workgroups, and for the deep kernel to one more
   // workgroup for every CU.  No slice is shorter than four row tiles, and the slices of
   // sinks take half a gigabyte at most.
   const int64_t bh = max64((int64_t)a->B * a->Hkv, 1), plain = bh * (a->nktiles - a->nsink);
