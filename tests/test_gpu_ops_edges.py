@@ -111,3 +111,24 @@ def test_many_heads_on_one_key_head(name, case, monkeypatch):
     torch.cuda.synchronize()
     check_forward(o, lse, r, "bf16", name)
     check_backward(dq, dk, dv, r, "bf16", name)
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "f16"])
+@pytest.mark.parametrize("name,case", [
+    ("uneven_ragged", (3, 4, 2, 300, 300, 128, -1, 0, 0, [300, 1, 130], [300, 40, 131])),
+    ("uneven_right", (2, 3, 3, 260, 260, 64, 0, -1, 0, None, [260, 100])),
+    ("uneven_long_axis", (3, 4, 2, 40, 3001, 128, -1, 0, 5, [40, 3, 0], [3001, 2000, 10])),
+    ("uneven_sinks", (2, 6, 3, 700, 700, 128, 400, 0, 130, [700, 513], [700, 513])),
+])
+def test_walks_of_uneven_length(name, case, dtype, monkeypatch):
+    """Tiles that are dealt out, longest first, over sequences of several lengths."""
+    import torch
+    monkeypatch.setitem(CASES, name, case)
+    x, lens, win, clipped = make(name, dtype, seed=13)
+    r = expect(x, win, clipped)
+    o, lse, dq, dk, dv = sentinels(x)
+    bsa.window_forward(x["q"], x["k"], x["v"], *win, o=o, lse=lse, **lens)
+    bsa.window_backward(x["q"], x["k"], x["v"], o, lse, x["do"], *win, dq=dq, dk=dk, dv=dv, **lens)
+    torch.cuda.synchronize()
+    check_forward(o, lse, r, dtype, name)
+    check_backward(dq, dk, dv, r, dtype, name)
