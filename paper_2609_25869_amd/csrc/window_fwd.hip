@@ -593,6 +593,9 @@ void window_fwd_piped_kernel(WindowArgs a) {
 // four slices in flight per thread.  One wave does for eight slices; more are shared by
 // the four waves of a workgroup (65536 keys in 512 slices: 37 us with a wave per row, 32
 // with four; 2048 rows of two slices: 27 us with a wave per row, 29 with four).
+//
+// A slice whose weight is 0 in 32 bits hands on what is not finite in it: its keys are
+// seen, and their weight is above 0.  (Slices of no visible key hold zeros.)
 template <typename T, int D, int W>
 __global__ __launch_bounds__(256) void window_join_kernel(WindowArgs a) {
   constexpr int kCols = D / 4, kPar = 64 * W / kCols, kBatch = 4;
@@ -633,7 +636,12 @@ __global__ __launch_bounds__(256) void window_join_kernel(WindowArgs a) {
     }
 #pragma unroll
     for (int i = 0; i < kBatch; ++i)
-      if (f[i] != 0.f) acc += f[i] * v[i];
+      if (f[i] != 0.f) {
+        acc += f[i] * v[i];
+      } else if (s0 + i * kPar < a.nsplit) {
+#pragma unroll
+        for (int e = 0; e < 4; ++e) acc[e] += fabsf(v[i][e]) < __builtin_huge_valf() ? 0.f : v[i][e];
+      }
   }
 #pragma unroll
   for (int x = kCols; x < 64; x <<= 1) {
