@@ -92,7 +92,9 @@ BSA_API bsa_status bsa_rope(const bsa_rope_shapes* shapes, const double* freq, c
  * `sinks` keys those with j <= p + right as well:
  *     O = softmax(scale * Q K^T over the visible keys) V.
  * A query that sees no key gets O = 0 and LSE = -inf.  heads is a multiple of
- * kv_heads; query head h reads key head h / (heads / kv_heads).
+ * kv_heads; query head h reads key head h / (heads / kv_heads).  The token
+ * strides of K and V, and in the backward pass of Q and dout, are below 2^23
+ * elements where there is more than one token.
  */
 typedef struct {
   int32_t batch, heads, kv_heads, seq_q, seq_kv, head_dim, dtype;

@@ -73,6 +73,9 @@ bsa_status check_tensor(const Tensor& t, int64_t size) {
 }
 
 Strides strides(const int64_t* s) { return Strides{s[0], s[1], s[2]}; }
+// For tensors whose token rows are loaded in tiles: the stride of an axis of one token
+// says nothing, and a row's length in its place keeps the tile's other rows out of bounds.
+Strides tile_strides(const int64_t* s, int64_t tokens, int64_t d) { return Strides{s[0], s[1], tokens > 1 ? s[2] : d}; }
 
 // ---------------------------------------------------------------- window
 bsa_status check_window(const bsa_window_shapes* sp) {
@@ -95,16 +98,17 @@ bsa_status check_window(const bsa_window_shapes* sp) {
 }
 
 // Tiles are addressed with 32 bits from their first row on.
-bsa_status check_tile_stride(const char* name, int64_t stride) {
-  if (stride >= (int64_t(1) << 23)) return fail(BSA_ERR_UNSUPPORTED, "token stride of %s is 2^23 elements or more", name);
+bsa_status check_tile_stride(const char* name, int64_t stride, int64_t tokens) {
+  if (tokens > 1 && stride >= (int64_t(1) << 23))
+    return fail(BSA_ERR_UNSUPPORTED, "token stride of %s is 2^23 elements or more", name);
   return BSA_OK;
 }
 
 WindowArgs window_args(const bsa_window_shapes& s) {
   WindowArgs a{};
-  a.qs = strides(s.q_stride);
-  a.ks = strides(s.k_stride);
-  a.vs = strides(s.v_stride);
+  a.qs = tile_strides(s.q_stride, s.seq_q, s.head_dim);
+  a.ks = tile_strides(s.k_stride, s.seq_kv, s.head_dim);
+  a.vs = tile_strides(s.v_stride, s.seq_kv, s.head_dim);
   a.os = strides(s.o_stride);
   a.B = s.batch;
   a.H = s.heads;
@@ -284,8 +288,8 @@ bsa_status bsa_window_forward(const bsa_window_shapes* shapes, const void* q, co
   TRY(check_tensor({"o", o, s.o_stride, s.batch, s.heads, s.seq_q, s.head_dim, true}, 2));
   TRY(check_tensor({"k", k, s.k_stride, s.batch, s.kv_heads, s.seq_kv, s.head_dim, false}, 2));
   TRY(check_tensor({"v", v, s.v_stride, s.batch, s.kv_heads, s.seq_kv, s.head_dim, false}, 2));
-  TRY(check_tile_stride("k", s.k_stride[2]));
-  TRY(check_tile_stride("v", s.v_stride[2]));
+  TRY(check_tile_stride("k", s.k_stride[2], s.seq_kv));
+  TRY(check_tile_stride("v", s.v_stride[2], s.seq_kv));
   TRY(check_apart("o", o, {q, k, v}));
   WindowArgs a = window_args(s);
   TRY(check_workspace(window_bytes(a, s.head_dim, false), workspace, workspace_bytes));
@@ -318,10 +322,10 @@ bsa_status bsa_window_backward(const bsa_window_shapes* shapes, const bsa_window
   TRY(check_tensor({"v", v, s.v_stride, s.batch, s.kv_heads, s.seq_kv, s.head_dim, false}, 2));
   TRY(check_tensor({"dk", dk, g.dk_stride, s.batch, s.kv_heads, s.seq_kv, s.head_dim, true}, 2));
   TRY(check_tensor({"dv", dv, g.dv_stride, s.batch, s.kv_heads, s.seq_kv, s.head_dim, true}, 2));
-  TRY(check_tile_stride("q", s.q_stride[2]));
-  TRY(check_tile_stride("dout", g.do_stride[2]));
-  TRY(check_tile_stride("k", s.k_stride[2]));
-  TRY(check_tile_stride("v", s.v_stride[2]));
+  TRY(check_tile_stride("q", s.q_stride[2], s.seq_q));
+  TRY(check_tile_stride("dout", g.do_stride[2], s.seq_q));
+  TRY(check_tile_stride("k", s.k_stride[2], s.seq_kv));
+  TRY(check_tile_stride("v", s.v_stride[2], s.seq_kv));
   TRY(check_apart("dq", dq, {q, k, v, o, dout, dk, dv}));
   TRY(check_apart("dk", dk, {q, k, v, o, dout, dv}));
   TRY(check_apart("dv", dv, {q, k, v, o, dout}));
@@ -336,7 +340,7 @@ bsa_status bsa_window_backward(const bsa_window_shapes* shapes, const bsa_window
   a.dq = dq;
   a.dk = dk;
   a.dv = dv;
-  a.dos = strides(g.do_stride);
+  a.dos = tile_strides(g.do_stride, s.seq_q, s.head_dim);
   a.dqs = strides(g.dq_stride);
   a.dks = strides(g.dk_stride);
   a.dvs = strides(g.dv_stride);
