@@ -131,8 +131,10 @@ BSA_API bsa_status bsa_window_workspace(const bsa_window_shapes* shapes, int32_t
  * Probabilities are rounded to the tensors' type for their product with V; their
  * sum, the maximum and O are 32 bits (O before its division by the sum: values
  * of V of 2^127 / (256 kv_len) and more may overflow it).  Values of K and V
- * that are not finite reach the queries that see them and no others.  Results do not depend on the
- * order in which workgroups run.
+ * that are not finite reach the queries that see them and no others.  (Rows that
+ * meet such a value of V are formed a second time: up to twelve times the time
+ * of the call, if they are all of them.)  Results do not depend on the order in
+ * which workgroups run.
  */
 BSA_API bsa_status bsa_window_forward(const bsa_window_shapes* shapes, const void* q, const void* k, const void* v,
                                       void* o, float* lse, const int32_t* q_len, const int32_t* kv_len,

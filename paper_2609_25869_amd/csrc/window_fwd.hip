@@ -35,50 +35,89 @@ __device__ inline float max3(float a, float b, float c) {
   return r;
 }
 
-// O of one row again, unnormalised, from the keys it sees alone: the wave takes them
-// four at a time, a lane D / 64 columns.  The products of a tile add 0 times V for the
-// keys that a row does not see, which is NaN where V is not finite; rows that come out
-// so are formed again here.  (A row that sees NaN in every column ends at that key.)
+// O of the rows `mine` of a wave again, unnormalised, in place of o.  The products of a
+// tile add 0 times V for the keys that a row does not see, which is NaN where V is not
+// finite; rows that come out so are formed again here, with such values taken out of the
+// products (0 in their place).  What a row sees of them is added from a product of its own:
+// 1 for a visible key, else 0, times 1 for infinity, 32 for -infinity and 33 for NaN.  Its
+// sums over 16 keys are whole numbers that both types and 32 bits hold, and tell the three
+// apart.  (A key whose score is -inf has no weight and adds nothing.)
+//
+// A lane reads its own elements of K and V from memory: the other waves of the workgroup
+// may have ended, so there is no barrier, and the ring is not touched.  (28800 queries, 24
+// heads of 128, 14401 keys around each and 3600 sinks: 4.9 ms, with one infinity in the
+// first value of every head 34 ms, with one in every value 39, of infinities alone 55.)
 template <typename T, int D, int TK>
-__device__ inline void row_alone(const WindowArgs& a, const KeyTiles& kt, int t_begin, int t_end, int b, int kvh, int qi,
-                                 int qh, int lo, int hi, float m, int lane, float* acc) {
-  constexpr int C = D / 64;
-  const T* q = static_cast<const T*>(a.q) + b * a.qs.b + qh * a.qs.h + qi * a.qs.n + C * lane;
-  const T* k = static_cast<const T*>(a.k) + b * a.ks.b + kvh * a.ks.h + C * lane;
-  const T* v = static_cast<const T*>(a.v) + b * a.vs.b + kvh * a.vs.h + C * lane;
-  float qv[C];
+__device__ inline void rows_again(const WindowArgs& a, const KeyTiles& kt, int t_begin, int t_end, int b, int kvh, int qi,
+                                  int qh, int lo, int hi, float m, bool mine, int lane, f32x16* o) {
+  using E = Elem<T>;
+  using R = Rows<D>;
+  typedef typename E::x8 x8;
+  const int n = lane & 31, hh = lane >> 5;
+  const T* q = static_cast<const T*>(a.q) + b * a.qs.b + qh * a.qs.h + qi * a.qs.n + 8 * hh;
+  const T* k = static_cast<const T*>(a.k) + b * a.ks.b + kvh * a.ks.h + 8 * hh;
+  const T* v = static_cast<const T*>(a.v) + b * a.vs.b + kvh * a.vs.h + n;
+  const float ref = m == kNegInf ? 0.f : m;
 #pragma unroll
-  for (int c = 0; c < C; ++c) {
-    qv[c] = (float)q[c];
-    acc[c] = 0.f;
+  for (int d = 0; d < R::kBlocks; ++d) {
+#pragma unroll
+    for (int i = 0; i < 16; ++i) o[d][i] = mine ? 0.f : o[d][i];
   }
   for (int t = t_begin; t < t_end; ++t) {
-    const int j0 = kt.key<TK>(t), j1 = min(min(j0 + TK, kt.limit(t)), hi + 1);
-    for (int j = j0; j < j1; j += 4) {
-      float s[4], vv[4][C];
+    const int end = kt.limit(t);  // of the tile's keys
+    for (int j0 = kt.key<TK>(t), jt = min(j0 + TK, end); j0 < jt; j0 += 32) {
+      const uint32_t bits = mine ? visible_bits(j0, lo, min(hi, end - 1), a.sinks) : 0u;
+      if (__ballot(bits != 0) == 0) continue;
+      f32x16 s = {};
 #pragma unroll
-      for (int i = 0; i < 4; ++i) {
-        const int key = j + i;
-        s[i] = kNegInf;
-        if (key >= j1 || (key < lo && key >= a.sinks)) continue;
-        float dot = 0.f;
+      for (int c = 0; c < R::kSteps; ++c) {
+        x8 kf = {};
+        if (j0 + n < end) kf = *reinterpret_cast<const x8*>(k + (j0 + n) * a.ks.n + 16 * c);
+        s = E::mfma(kf, *reinterpret_cast<const x8*>(q + 16 * c), s);
+      }
+      u32x4 p[2], one[2];
 #pragma unroll
-        for (int c = 0; c < C; ++c) {
-          dot += qv[c] * (float)k[key * a.ks.n + c];
-          vv[i][c] = (float)v[key * a.vs.n + c];
+      for (int i = 0; i < 16; i += 2) {
+        const uint32_t see = bits >> (4 * hh + (i >> 2) * 8 + (i & 3));
+        const bool s0 = (see & 1u) && s[i] > kNegInf, s1 = (see & 2u) && s[i + 1] > kNegInf;
+        p[i / 8][(i % 8) / 2] = pack2<T>(s0 ? fast_exp2(__builtin_fmaf(s[i], a.scale_log2, -ref)) : 0.f,
+                                         s1 ? fast_exp2(__builtin_fmaf(s[i + 1], a.scale_log2, -ref)) : 0.f);
+        one[i / 8][(i % 8) / 2] = pack2<T>(s0 ? 1.f : 0.f, s1 ? 1.f : 0.f);
+      }
+#pragma unroll
+      for (int c = 0; c < 2; ++c) {
+        x8 x[R::kBlocks];  // V by columns, its 16 keys in the order that the probabilities have
+#pragma unroll
+        for (int e = 0; e < 8; ++e) {
+          const int key = j0 + 16 * c + 8 * (e >> 2) + 4 * hh + (e & 3);
+#pragma unroll
+          for (int d = 0; d < R::kBlocks; ++d) x[d][e] = key < end ? v[key * a.vs.n + 32 * d] : (T)0.f;
         }
 #pragma unroll
-        for (int x = 32; x; x >>= 1) dot += __shfl_xor(dot, x);
-        s[i] = dot;
-      }
+        for (int d = 0; d < R::kBlocks; ++d) {
+          bool bad = false;
 #pragma unroll
-      for (int i = 0; i < 4; ++i) {
-        if (s[i] == kNegInf) continue;
-        const float p = fast_exp2(__builtin_fmaf(s[i], a.scale_log2, -m));
+          for (int e = 0; e < 8; ++e) bad |= !(fabsf((float)x[d][e]) < __builtin_huge_valf());
+          if (__ballot(bad) != 0) {
+            x8 code;
 #pragma unroll
-        for (int c = 0; c < C; ++c) acc[c] += p * vv[i][c];
+            for (int e = 0; e < 8; ++e) {
+              const float f = (float)x[d][e];
+              const bool fin = fabsf(f) < __builtin_huge_valf();
+              code[e] = (T)(fin ? 0.f : f > 0.f ? 1.f : f < 0.f ? 32.f : 33.f);
+              x[d][e] = fin ? x[d][e] : (T)0.f;
+            }
+            const f32x16 sees = E::mfma(code, __builtin_bit_cast(x8, one[c]), f32x16{});
+#pragma unroll
+            for (int i = 0; i < 16; ++i) {
+              const int w = (int)sees[i];
+              if (w & 31) o[d][i] += __builtin_huge_valf();
+              if (w >> 5) o[d][i] += kNegInf;
+            }
+          }
+          o[d] = E::mfma(x[d], __builtin_bit_cast(x8, p[c]), o[d]);
+        }
       }
-      if (__ballot(acc[0] == acc[0] || acc[C - 1] == acc[C - 1]) == 0) return;
     }
   }
 }
@@ -86,11 +125,10 @@ __device__ inline void row_alone(const WindowArgs& a, const KeyTiles& kt, int t_
 // Ends a wave's work: O and LSE of its rows, or the state of its slice of the keys
 // for the join.
 template <typename T, int D, int TK>
-__device__ inline void store_rows(const WindowArgs& a, const KeyTiles& kt, int t_begin, int t_end, const f32x16* o, float m,
+__device__ inline void store_rows(const WindowArgs& a, const KeyTiles& kt, int t_begin, int t_end, f32x16* o, float m,
                                   float l, bool live, int lo, int hi, int b, int bh, int qi, int qh, int row, int split,
                                   int lane) {
   using R = Rows<D>;
-  constexpr int C = D / 64;
   const int hh = lane >> 5;
   l += other_half(l, lane);
   float zero = 0.f;  // NaN where a column is not finite
@@ -100,9 +138,11 @@ __device__ inline void store_rows(const WindowArgs& a, const KeyTiles& kt, int t
     for (int i = 0; i < 16; ++i) zero = __builtin_fmaf(o[d][i], 0.f, zero);
   }
   // (a sum that is not finite itself says that the row saw such a key)
-  uint64_t again = __ballot(live && zero != 0.f && l < __builtin_huge_valf());
-  uint32_t redo = (uint32_t)again | (uint32_t)(again >> 32);
-  const bool mine = !((redo >> (lane & 31)) & 1u);
+  const uint64_t again = __ballot(live && zero != 0.f && l < __builtin_huge_valf());
+  if (__builtin_expect(again != 0, 0)) {
+    const uint32_t rows = (uint32_t)again | (uint32_t)(again >> 32);
+    rows_again<T, D, TK>(a, kt, t_begin, t_end, b, bh % a.Hkv, qi, qh, lo, hi, m, (rows >> (lane & 31)) & 1u, lane, o);
+  }
   const float inv = l == 0.f ? 0.f : 1.f / l;
   const int64_t rows = (int64_t)a.B * a.Hkv * a.Nq * a.group;
   // state of a slice: [row][slice] of O, then of (m, l)
@@ -118,7 +158,7 @@ __device__ inline void store_rows(const WindowArgs& a, const KeyTiles& kt, int t
           u32x2 v;
           v[0] = pack2<T>(o[d][4 * g] * inv, o[d][4 * g + 1] * inv);
           v[1] = pack2<T>(o[d][4 * g + 2] * inv, o[d][4 * g + 3] * inv);
-          if (mine) *reinterpret_cast<u32x2*>(op + d * 32 + 8 * g + 4 * hh) = v;
+          *reinterpret_cast<u32x2*>(op + d * 32 + 8 * g + 4 * hh) = v;
         }
       }
       if (a.lse && hh == 0) a.lse[((int64_t)b * a.H + qh) * a.Nq + qi] = l == 0.f ? kNegInf : (m + __log2f(l)) * kLn2;
@@ -127,24 +167,10 @@ __device__ inline void store_rows(const WindowArgs& a, const KeyTiles& kt, int t
       for (int d = 0; d < R::kBlocks; ++d) {
 #pragma unroll
         for (int g = 0; g < 4; ++g)
-          if (mine)
-            *reinterpret_cast<f32x4*>(po + d * 32 + 8 * g + 4 * hh) =
-                f32x4{o[d][4 * g], o[d][4 * g + 1], o[d][4 * g + 2], o[d][4 * g + 3]};
+          *reinterpret_cast<f32x4*>(po + d * 32 + 8 * g + 4 * hh) =
+              f32x4{o[d][4 * g], o[d][4 * g + 1], o[d][4 * g + 2], o[d][4 * g + 3]};
       }
       if (hh == 0) *reinterpret_cast<f32x2*>(a.part + rows * a.nsplit * D + 2 * at) = f32x2{m, l};
-    }
-  }
-  for (; __builtin_expect(redo != 0, 0); redo &= redo - 1) {
-    const int r = __ffs(redo) - 1;
-    const int qi1 = __shfl(qi, r), qh1 = __shfl(qh, r), row1 = __shfl(row, r);
-    float acc[C];
-    row_alone<T, D, TK>(a, kt, t_begin, t_end, b, bh % a.Hkv, qi1, qh1, __shfl(lo, r), __shfl(hi, r), __shfl(m, r), lane, acc);
-    const float f = __shfl(inv, r);
-#pragma unroll
-    for (int c = 0; c < C; ++c) {
-      const int col = C * lane + c;
-      if (a.nsplit == 1) (static_cast<T*>(a.o) + b * a.os.b + qh1 * a.os.h + qi1 * a.os.n)[col] = (T)(acc[c] * f);
-      else a.part[(((int64_t)bh * a.Nq * a.group + row1) * a.nsplit + split) * D + col] = acc[c];
     }
   }
 }
