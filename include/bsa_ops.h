@@ -148,9 +148,10 @@ BSA_API bsa_status bsa_window_forward(const bsa_window_shapes* shapes, const voi
  * that no query sees get 0.  Sums are taken in a fixed order (no atomics).
  * Probabilities and the scores' gradients are rounded to the tensors' type for
  * their products; float16 holds the latter to 2^-25 below 2^-14, so the loss is
- * scaled where they are smaller.  Rows behind a sequence's end and keys that no
- * query sees are never read, but a value that is not finite anywhere else may
- * reach the gradients of neighbouring rows and keys that it is not visible to.
+ * scaled where they are smaller.  What the rows behind a sequence's end and the
+ * keys that no query sees hold does not affect results, but a value that is not
+ * finite anywhere else may reach the gradients of neighbouring rows and keys that
+ * it is not visible to.
  */
 BSA_API bsa_status bsa_window_backward(const bsa_window_shapes* shapes, const bsa_window_grads* grads, const void* q,
                                        const void* k, const void* v, const void* o, const float* lse,
