@@ -5,7 +5,8 @@ functions.  Tensors are CUDA tensors [B, N, H, d] with d contiguous and 16-byte
 aligned rows.  Work runs on the tensors' device, on its current stream unless
 one is given; outputs and workspaces that are not passed in are allocated for
 that stream.  Nothing here takes part in autograd: backward passes are calls of
-their own (rope with inverse=True, window_backward).
+their own (rope with inverse=True, window_backward), and a call on tensors that
+require gradients while torch records them warns that its results have none.
 
 A call of a few microseconds on the device is bound by what the host does for
 it, so the checks take each tensor's properties once, the shape structures are
@@ -19,6 +20,7 @@ import contextlib
 import ctypes
 import functools
 import struct
+import warnings
 from typing import Optional, Sequence, Tuple
 
 from . import _ops_ffi
@@ -105,6 +107,13 @@ def _run(device, stream, call):
         return call(handle)
 
 
+def _not_recorded(name, backward):
+    """Warns at the caller's line that a call's results carry no gradients."""
+    if torch.is_grad_enabled():
+        warnings.warn("%s takes no part in autograd: no gradient reaches its inputs through its results (%s gives it; "
+                      "call this under torch.no_grad())" % (name, backward), stacklevel=3)
+
+
 # ----------------------------------------------------------------------------
 # Rotary positions
 
@@ -137,7 +146,8 @@ def rope(q, k=None, v=None, *, freq, pairs: Sequence[int], interleaved: bool = T
     sequences' first tokens go to (new tokens of a cache [B, capacity, Hkv, d]);
     v is copied there unturned.  inverse=True turns back: the backward pass on
     gradients.  out_q may be q, and out_k k.  Returns the outputs of the tensors
-    given, allocated where they are not passed in (zeros behind `lengths`)."""
+    given, allocated where they are not passed in (zeros behind `lengths`).
+    They carry no gradients: autograd does not record the call."""
     dev, dtype, code = _first("q", q)
     qs = _rows("q", q, dev, dtype)
     B, N, H, d = q_shape = q.shape
@@ -177,6 +187,8 @@ def rope(q, k=None, v=None, *, freq, pairs: Sequence[int], interleaved: bool = T
         raise ValueError("give either positions or grid")
     else:
         (g0, g1, g2), (o0, o1, o2) = grid, origin
+    if q.requires_grad or (k is not None and k.requires_grad) or (v is not None and v.requires_grad):
+        _not_recorded("rope", "rope with inverse=True")
     len_ptr, row_ptr = _ints("lengths", lengths, dev, B), _ints("rows", rows, dev, B)
     if rows is not None and (out_k is None or (v is not None and out_v is None)):
         raise ValueError("rows needs the caches as out_k (and out_v)")
@@ -277,8 +289,12 @@ def window_forward(q, k, v, left: int, right: int = 0, sinks: int = 0, *, scale:
     first `sinks` keys those up to p + right.  q_len and kv_len are int32 [B] on
     the device (default: Nq, Nkv).  Returns (o, lse), lse float32 [B, H, Nq]; a
     query that sees nothing gets o = 0 and lse = -inf.  Rows of a given o and
-    lse from q_len on keep what they held; allocated ones hold zeros there."""
+    lse from q_len on keep what they held; allocated ones hold zeros there.
+    o and lse carry no gradients: autograd does not record the call, and
+    window_backward returns them."""
     dev, dtype, q_shape, _, fields = _window_head(q, k, v, left, right, sinks, scale)
+    if q.requires_grad or k.requires_grad or v.requires_grad:
+        _not_recorded("window_forward", "window_backward")
     B, Nq, H, _ = q_shape
     ql, kl = _ints("q_len", q_len, dev, B), _ints("kv_len", kv_len, dev, B)
 
@@ -304,7 +320,8 @@ def window_backward(q, k, v, o, lse, do, left: int, right: int = 0, sinks: int =
     """Gradients (dq, dk, dv) of window_forward for the gradient `do` of o
     (bsa_window_backward), with the o and lse that it returned and its other
     arguments unchanged.  Rows of given dq from q_len on, and of dk and dv from
-    kv_len on, keep what they held; allocated ones hold zeros there."""
+    kv_len on, keep what they held; allocated ones hold zeros there.  The
+    gradients carry none of their own."""
     dev, dtype, q_shape, k_shape, fields = _window_head(q, k, v, left, right, sinks, scale)
     B, Nq, H, _ = q_shape
     os, gs = _rows("o", o, dev, dtype, q_shape), _rows("do", do, dev, dtype, q_shape)
