@@ -125,7 +125,11 @@ WindowArgs window_args(const bsa_window_shapes& s) {
   // better read by one XCD.  (8192 tokens, all keys before, forward, dQ, dK and dV: 12
   // heads 1109 us in shares from the first tile on, 915 dealt out; 32 heads 2412 and 2290
   // with the longest first.  40 sequences of 2048 tokens, 2 key heads: 1300 and 945 with
-  // shares that move on from sequence to sequence.)
+  // shares that move on from sequence to sequence.)  At the limits, forward, dQ, dK and dV:
+  // 60 heads in all (5 sequences of 2048) 454 us in shares and 390 dealt out, 64 heads 484
+  // and 377; 66 heads 494 and 416, 100 heads 667 and 602, so up to there short sequences
+  // would still gain; 96 heads of 8192 tokens 7040 and 7390, 300 heads of 2048 1810 and
+  // 1835.  kv_heads a multiple of 8: 8 heads of 8192 730 and 752, 16 heads 1203 and 1214.
   const bool far_left = 2 * (int64_t)a.left > s.seq_kv, far_right = 2 * (int64_t)a.right > s.seq_kv;
   a.deal = far_left != far_right && s.kv_heads % 8 != 0 && (int64_t)s.batch * s.kv_heads <= 64;
   a.later_longer = far_left && !far_right;

@@ -12,7 +12,12 @@
 // radians).
 //
 // The work is the memory traffic: every element is read and written once (115200 tokens,
-// Q and K of 24 heads of 128 in bfloat16: 492 us, 5.8 TB/s read and written).
+// Q and K of 24 heads of 128 in bfloat16: 492 us, 5.8 TB/s read and written; a prompt of
+// 32768 tokens, 32 and 8 heads of 128, by positions: 137 us in the half layout, 4.9 TB/s,
+// 140 interleaved).  One pair a thread, where P is no multiple of eight, moves single
+// elements: 171 us with 60 pairs.  One token takes 5.3 us, of which 3.8 are left without
+// pairs: the kernel's start, and a row's way through memory and back; the rest is a
+// thread's eight sines, formed from 64-bit products.
 #include "ops_internal.h"
 
 namespace bsa_ops {

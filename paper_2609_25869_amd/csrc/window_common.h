@@ -1,8 +1,8 @@
 // Device helpers of the window attention kernels: element types, matrix
 // instructions, tiles in LDS and the visibility of keys.
 //
-// A tile is 8 KB or less of token rows, row-major, 2 * D bytes a row, filled by
-// loads that go straight from memory to LDS.  The 16-byte chunks of row r are
+// A tile is 8 or 16 KB of token rows (32 or 64 of them), row-major, 2 * D bytes a row,
+// filled by loads that go straight from memory to LDS.  The 16-byte chunks of row r are
 // stored at chunk ^ swizzle(r), so that both ways of reading it - 32 rows at one
 // chunk for the operands that contract over the head dim, and four rows of
 // four chunks through the transposing read for those that contract over the
@@ -20,7 +20,6 @@ namespace bsa_ops {
 namespace {
 
 typedef short i16x4 __attribute__((ext_vector_type(4)));
-typedef short i16x8 __attribute__((ext_vector_type(8)));
 typedef float f32x2 __attribute__((ext_vector_type(2)));
 typedef float f32x4 __attribute__((ext_vector_type(4)));
 typedef float f32x16 __attribute__((ext_vector_type(16)));
@@ -71,13 +70,6 @@ template <int N>
 __device__ inline void wait_vm_lgkm() {
   static_assert(N >= 0 && N < 64, "vmcnt range");
   __builtin_amdgcn_s_waitcnt(0x0070 | (N & 15) | ((N >> 4) << 14));
-}
-
-// The same for vector memory alone.
-template <int N>
-__device__ inline void wait_vm() {
-  static_assert(N >= 0 && N < 64, "vmcnt range");
-  __builtin_amdgcn_s_waitcnt(0x0F70 | (N & 15) | ((N >> 4) << 14));
 }
 
 // Workgroup barrier without a memory fence: what the LDS loads wrote is complete
@@ -202,7 +194,7 @@ __device__ inline uint32_t visible_bits(int j, int lo, int hi, int sinks) {
 }
 
 template <int D>
-constexpr int kTileKeys = 4096 / D;  // 8 KB of K: 32 keys of 128 elements, 64 of 64
+constexpr int kTileKeys = 4096 / D;  // window_fwd_kernel's, 8 KB of K: 32 keys of 128 elements, 64 of 64
 
 // The keys of one row tile as a list of tiles: `ns` tiles of sinks from key 0, then
 // tiles from key w0 on.  Keys that no row of the tile sees are in none: rows from

@@ -1,12 +1,17 @@
 // Window attention forward for gfx950: a workgroup of NW waves owns 32 * NW rows
 // (query tokens x the heads that share a key head), each wave 32 of them, and
 // walks the keys that any of them sees - the first `sinks` and one contiguous
-// range - in tiles of 8 KB of K and 8 KB of V that come straight from memory to a
-// ring in LDS.
+// range - in tiles of 8 or 16 KB of K and as much of V that come straight from memory
+// to a ring in LDS.
 //
 // Scores are computed transposed, S^T = K Q^T (v_mfma 32x32x16): a lane then owns
 // one row and 16 keys of each 32, so the softmax state is one number per lane and
 // O^T += V^T P^T takes the lane's own probabilities as its operand.
+//
+// P is rounded to the tensors' type for that product, whose operands the matrix unit
+// takes in 16 bits: each weight is off by half a step at most, which adds 0.001
+// (relative, root mean square, bf16) to the 0.0017 of the rounding of O itself.  The sum
+// is that of the weights before.
 #include "window_common.h"
 
 // (Kernel bodies are kept from the host's pass, which drops the launch stub of a
@@ -617,8 +622,9 @@ void window_fwd_piped_kernel(WindowArgs a) {
 
 // Joins the slices of a row: W waves per row, D / 4 threads a slice, with the loads of
 // four slices in flight per thread.  One wave does for eight slices; more are shared by
-// the four waves of a workgroup (65536 keys in 512 slices: 37 us with a wave per row, 32
-// with four; 2048 rows of two slices: 27 us with a wave per row, 29 with four).
+// the four waves of a workgroup (one row of 256 slices: 28 us with a wave per row, 12 with
+// four; 128 rows of 16: 5.8 and 4.4; 1024 rows of eight: 4.7 and 4.8; 2048 rows of two:
+// 4.1 and 5.4).
 //
 // A slice whose weight is 0 in 32 bits hands on what is not finite in it: its keys are
 // seen, and their weight is above 0.  (Slices of no visible key hold zeros.)
@@ -726,7 +732,8 @@ hipError_t launch(const WindowArgs& a, const ForwardPlan& p, hipStream_t s) {
 // head dim 128, so slices are weighed: a tile of 64 keys takes a workgroup 1.2 us (1.74
 // with two on a CU), the join 4 us and 27 ns a slice and workgroup.  (96 row tiles of 504
 // keys: 16.5 us whole, 29.7 in five slices; 3 row tiles of 8000 keys: 65 us in two
-// slices, 20 in forty.)
+// slices, 20 in forty.)  These are head dim 128's; at 64 a tile takes 1.1 us (1.3 with two
+// on a CU, 1.8 with three, 2.3 with four), near enough that the same weighing serves.
 ForwardPlan plan_forward(const WindowArgs& a, int d) {
   ForwardPlan p{};
   const int64_t rows = (int64_t)a.Nq * a.group;
