@@ -138,10 +138,19 @@ __device__ inline void scale_inplace(f32x16& v, float alpha) {
   }
 }
 
-// x = keep ? x : -inf, in place (keep is per lane)
-__device__ inline void mask_inplace(float& x, bool keep) {
+// The lanes with `keep`, ready to be read by inline asm: a vector instruction may read a
+// scalar register two wait states after a comparison has written it, and the compiler
+// keeps that distance for its own instructions only.
+__device__ inline uint64_t lanes_of(bool keep) {
+  uint64_t m = __ballot(keep);
+  asm volatile("s_nop 1" : "+s"(m));
+  return m;
+}
+
+// x = (the lane is in keep) ? x : -inf, in place; keep comes from lanes_of
+__device__ inline void mask_inplace(float& x, uint64_t keep) {
   const float ninf = -__builtin_huge_valf();
-  asm volatile("v_cndmask_b32_e64 %0, %1, %0, %2" : "+v"(x) : "v"(ninf), "s"(__ballot(keep)));
+  asm volatile("v_cndmask_b32_e64 %0, %1, %0, %2" : "+v"(x) : "v"(ninf), "s"(keep));
 }
 
 // A row's reference is raised only when the probabilities of a tile, formed
@@ -472,7 +481,7 @@ void attn_fwd_kernel(AttnArgs a) {
       for (int i = 0; i < 16; ++i) {
         const int jc = kb * 32 + (i >> 2) * 8 + (i & 3);  // key index minus 4 * hh
         float x = s[kb][i];
-        mask_inplace(x, (mine >> jc) & 1ull);
+        mask_inplace(x, lanes_of((mine >> jc) & 1ull));
         s[kb][i] = x;
       }
     }
@@ -490,8 +499,9 @@ void attn_fwd_kernel(AttnArgs a) {
     bool any = false;
 #pragma unroll
     for (int blk = 0; blk < 4; ++blk) {
-      const bool keep = (row >> blk) & 1u;
-      any = any || keep;
+      const bool seen = (row >> blk) & 1u;
+      const uint64_t keep = lanes_of(seen);
+      any = any || seen;
 #pragma unroll
       for (int i = 0; i < 8; ++i) {
         float x = s[blk / 2][8 * (blk % 2) + i];
